@@ -209,6 +209,125 @@ hgf_status hgf_diff_attention_decode(const void *q_f16, const void *k_cache_f16,
                                      float lambda, void *out_f16, void *workspace, size_t workspace_bytes,
                                      void *stream);
 
+/* ---------------------------------------------------------------- differential attention over prompts
+ *
+ * The same attention for many query rows at a time (reading a prompt, scoring a batch, the next turn of a
+ * conversation): a packed batch of B sequences, the queries of sequence b in rows cu_q[b] .. cu_q[b+1]-1 of q, its keys and
+ * values in rows cu_k[b] .. cu_k[b+1]-1 of k and v.  The last query of a sequence stands at its last key: with nq queries
+ * and nk keys, query i has position p = nk - nq + i (nq < nk: rows behind earlier keys, as after
+ * hgf_kv8_gather; p < 0: a row with nothing before it).  For branch c and head h, key j of the same sequence:
+ *
+ *     x = q . k_j / sqrt(d_h);   s_j = (softcap > 0 ? softcap tanh(x / softcap) : x) - slope |p - j|
+ *     query i sees key j if   doc_q[i] == doc_k[j] >= 0 (with documents)
+ *                       and   j <= p  or  j < prefix[b] (causal; without prefix only j <= p; not causal: every j)
+ *     out = (softmax(s1) V - lambda softmax(s2) V) / 2, the sums over the keys that are seen; a row that sees none is zero.
+ *
+ *   q_f16        fp16 [Tq, 2 n_heads, d_h]    k_f16 fp16 [Tk, 2 n_heads, d_h]    v_f16 fp16 [Tk, n_heads, d_h]
+ *   cu_q, cu_k   int32 [B + 1] (device), rising, from 0 .. Tq and 0 .. Tk; cu_k NULL: cu_q (then Tk must be Tq).
+ *                Offsets beyond are clipped to the tensor, a sequence whose offsets fall has no rows
+ *   prefix       int32 [B] (device) or NULL: so many keys of the sequence are seen from every row
+ *   doc_q, doc_k int32 [Tq], int32 [Tk] (device), both or none: document numbers in any order; negative: padding, which sees
+ *                nothing and is not seen
+ *   softcap      0 (none) or positive
+ *   slopes       fp32 [2 n_heads] (device) or NULL: a distance bias per head of q
+ *   out_f16      fp16 [Tq, n_heads, d_h]; rows in front of cu_q[0] and behind cu_q[B] are left as they are
+ * d_h 16, 32, 64 or 128; n_heads <= 1024; Tq, Tk < 2^24.  fp32 scores and sums; the softmax weights are
+ * rounded to fp16 for the matrix cores.  What a row does not see does not change it, infinities and what is not a
+ * number in k and v included. */
+hgf_status hgf_diff_attention_prefill(const void *q_f16, const void *k_f16, const void *v_f16, const int32_t *cu_q,
+                                      const int32_t *cu_k, int B, int Tq, int Tk, int n_heads, int d_h, float lambda,
+                                      int causal, const int32_t *prefix, const int32_t *doc_q, const int32_t *doc_k,
+                                      float softcap, const float *slopes, void *out_f16, void *stream);
+
+/* ---------------------------------------------------------------- a paged cache in 8 bits
+ *
+ * Keys and values of many sequences in pages of `page` positions, at a little over half the bytes of an fp16 cache.  One
+ * hgf_kv8_pages holds which sequence has which pages; any number of caches (one for each layer of a model)
+ * use it together.  All arrays are the caller's device memory.
+ *
+ * 16 consecutive positions of one head share a scale, a power of two: the smallest 2^e (e >= -30) with 127 * 2^e >= the
+ * largest magnitude among them when they were written.  A code is round_half_even(x / 2^e).  When a later token of the 16 needs
+ * a larger scale, the codes that are there become round_half_even(code * old / new): whatever the
+ * order, a code is off by less than one step of its final scale (half a step where nothing grew), and the scale does not depend
+ * on how the tokens were split into calls.  What is not a number is stored as 0, an infinity as +-65504.
+ *
+ * Layout: page p of k_codes holds, head by head, its positions' codes in blocks of 16 positions, a block as d_h / 16 times
+ * 16 positions of 16 columns; v_codes likewise, a block as d_h columns of 16 positions: pieces of
+ * 16 bytes in the order in which the matrix cores take them. */
+typedef struct {
+    int n_pages;            /* 1 .. 2^24                                                                  */
+    int page;               /* positions per page: 16, 32, 64, 128 or 256                                 */
+    int n_seqs;             /* rows of the table, 1 .. 16384                                              */
+    int max_pages;          /* pages a sequence can have; max_pages * page <= 2^24                        */
+    int32_t *table;         /* [n_seqs, max_pages] page numbers, -1: none (to begin with: all -1)         */
+    int32_t *lens;          /* [n_seqs] positions of each sequence         (to begin with: all 0)         */
+    int32_t *refs;          /* [n_pages] how many sequences have the page, 0: free (to begin with: all 0); 16-byte aligned */
+} hgf_kv8_pages;
+
+typedef struct {
+    int n_pages, page;      /* as in hgf_kv8_pages                                                        */
+    int n_heads, d_h;       /* q, k: 2 n_heads heads, v: n_heads heads; d_h 16, 32, 64 or 128             */
+    int8_t *k_codes;        /* [n_pages, 2 n_heads, page / 16, d_h / 16, 16 positions, 16 columns]        */
+    float *k_scale;         /* [n_pages, 2 n_heads, page / 16]                                            */
+    int8_t *v_codes;        /* [n_pages, n_heads, page / 16, d_h columns, 16 positions]                   */
+    float *v_scale;         /* [n_pages, n_heads, page / 16]                                              */
+} hgf_kv8_cache;
+
+/* The operations on pages run on the device; new pages go to the requests in the order of their list, always the
+ * free one with the lowest number.  `seqs`, `src`, `dst`: int32 [n] sequence numbers (n <= 16384); ok_out int32 [n] receives 1, or
+ * 0 where a request was refused and changed nothing: a sequence outside 0 .. n_seqs-1 or one that the list names before
+ * (as seqs or dst), or not enough free pages left for it and those before it (requests that need none are still granted).
+ *
+ * grow: sequence seqs[i] becomes new_tokens[i] positions longer (refused: a negative number, or beyond max_pages pages);
+ *   the caller then writes them with hgf_kv8_append.
+ * fork: dst[i], which must be empty and not src[i], becomes what src[i] was before the call: it shares src's full pages, and where the last one is not full it gets
+ *   a page of its own; pairs_out[i] = (src's page, the new page), to be copied in every cache by hgf_kv8_copy_pages before
+ *   either sequence grows, or (-1, -1).
+ * free: the sequences become empty; pages that no sequence has any more are free.  (No ok_out: other numbers are passed over.)
+ * compact: the pages in use move to the lowest numbers (the k-th page in use behind their count goes to the k-th free page in
+ *   front of it), in table and refs; pairs_out (int32 [max(1, n_pages / 2), 2]) receives the moves in that order, then (-1, -1); count_out
+ *   int32 [1] their number; moved_out int32 [n_pages] the new number of every page, -1 for a free one.  No
+ *   page is both a source and a destination. */
+hgf_status hgf_kv8_pages_grow(const hgf_kv8_pages *pages, const int32_t *seqs, const int32_t *new_tokens, int n,
+                              int32_t *ok_out, void *stream);
+hgf_status hgf_kv8_pages_fork(const hgf_kv8_pages *pages, const int32_t *src, const int32_t *dst, int n,
+                              int32_t *pairs_out, int32_t *ok_out, void *stream);
+hgf_status hgf_kv8_pages_free(const hgf_kv8_pages *pages, const int32_t *seqs, int n, void *stream);
+hgf_status hgf_kv8_pages_compact(const hgf_kv8_pages *pages, int32_t *pairs_out, int32_t *count_out,
+                                 int32_t *moved_out, void *stream);
+
+/* Copies the contents (codes and scales) of page pairs[i][0] to page pairs[i][1], i < min(n, *count) (count NULL: n; both
+ * on the device).  Pairs with a number outside 0 .. n_pages-1, or with twice the same one, are passed over.  No page
+ * may be the destination of two pairs, or the source of one and the destination of another: such a page's contents are
+ * not defined afterwards. */
+hgf_status hgf_kv8_copy_pages(const hgf_kv8_cache *cache, const int32_t *pairs, const int32_t *count, int n, void *stream);
+
+/* In the calls below row b of the batch is sequence seqs[b] (int32 [B] on the device; NULL: sequence b, B <= n_seqs); rows whose
+ * number lies outside 0 .. n_seqs-1 are passed over.  lens beyond the table are clipped to it, and positions whose page
+ * number lies outside 0 .. n_pages-1 are not there: nothing is written to them, they are not attended to and read as zero.
+ *
+ * append: the new tokens of row b are the last ones of its sequence, positions lens - n .. lens - 1 (so the sequence
+ *   has been grown before); k_f16 [T, 2 n_heads, d_h], v_f16 [T, n_heads, d_h] hold them in rows cu_new[b] .. cu_new[b+1]-1
+ *   (int32 [B + 1], device, rising; NULL: one token each, T must be B).  Tokens in front of position 0 are dropped.  A
+ *   sequence may be named once per call.  Pages that a sequence shares are written for all that share them.
+ * gather: the inverse: the last cu[b+1] - cu[b] positions of row b as fp16 into rows cu[b] .. of k_f16 and v_f16 (all of a
+ *   sequence for cu[b+1] - cu[b] = lens); rows in front of position 0 become zero, rows outside cu[0] .. cu[B]-1 are left as they are. */
+hgf_status hgf_kv8_append(const void *k_f16, const void *v_f16, const hgf_kv8_cache *cache, const hgf_kv8_pages *pages,
+                          const int32_t *seqs, const int32_t *cu_new, int B, int T, void *stream);
+hgf_status hgf_kv8_gather(const hgf_kv8_cache *cache, const hgf_kv8_pages *pages, const int32_t *seqs, const int32_t *cu,
+                          int B, int T, void *k_f16, void *v_f16, void *stream);
+
+/* hgf_diff_attention_decode over such a cache: the newest token (position lens - 1, already appended) of every row attends to
+ * all positions of its sequence, with the softcap and slopes of hgf_diff_attention_prefill (|p - j| = lens - 1 - j).
+ *   q_f16     fp16 [B, 2 n_heads, d_h]       out_f16 fp16 [B, n_heads, d_h]; rows without positions become zero
+ *   workspace hgf_diff_attention_kv8_workspace_bytes(B, pages, n_heads, d_h) bytes, 16-byte aligned (0 bytes: may be NULL)
+ * The products are exact (q and the softmax weights as 23-bit fixed-point numbers against the codes in the integer matrix
+ * cores), statistics and sums are fp32. */
+size_t hgf_diff_attention_kv8_workspace_bytes(int B, const hgf_kv8_pages *pages, int n_heads, int d_h);
+hgf_status hgf_diff_attention_decode_kv8(const void *q_f16, const hgf_kv8_cache *cache, const hgf_kv8_pages *pages,
+                                         const int32_t *seqs, int B, float lambda, float softcap, const float *slopes,
+                                         void *out_f16, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- base-3 packing (1.6 bits per weight)
  *
  * The paper counts its backbone at log2 3 = 1.58 bits per weight (Sec. 4.1, Def. "Effective

@@ -32,6 +32,17 @@ class hgf_layer(ctypes.Structure):
                 ("ln_gamma", ctypes.c_void_p), ("ln_beta", ctypes.c_void_p), ("ln_eps", ctypes.c_float)]
 
 
+class hgf_kv8_pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("n_seqs", ctypes.c_int), ("max_pages", ctypes.c_int),
+                ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class hgf_kv8_cache(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("n_heads", ctypes.c_int), ("d_h", ctypes.c_int),
+                ("k_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -76,6 +87,27 @@ def lib() -> ctypes.CDLL:
     L.hgf_diff_attention_workspace_bytes.argtypes = [ci, ci, ci, ci]
     L.hgf_diff_attention_decode.restype = ci
     L.hgf_diff_attention_decode.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ctypes.c_float, vp, vp, sz, vp]
+    cf, pages, cache = ctypes.c_float, ctypes.POINTER(hgf_kv8_pages), ctypes.POINTER(hgf_kv8_cache)
+    L.hgf_diff_attention_prefill.restype = ci
+    L.hgf_diff_attention_prefill.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, cf, ci, vp, vp, vp, cf, vp, vp, vp]
+    L.hgf_kv8_pages_grow.restype = ci
+    L.hgf_kv8_pages_grow.argtypes = [pages, vp, vp, ci, vp, vp]
+    L.hgf_kv8_pages_fork.restype = ci
+    L.hgf_kv8_pages_fork.argtypes = [pages, vp, vp, ci, vp, vp, vp]
+    L.hgf_kv8_pages_free.restype = ci
+    L.hgf_kv8_pages_free.argtypes = [pages, vp, ci, vp]
+    L.hgf_kv8_pages_compact.restype = ci
+    L.hgf_kv8_pages_compact.argtypes = [pages, vp, vp, vp, vp]
+    L.hgf_kv8_copy_pages.restype = ci
+    L.hgf_kv8_copy_pages.argtypes = [cache, vp, vp, ci, vp]
+    L.hgf_kv8_append.restype = ci
+    L.hgf_kv8_append.argtypes = [vp, vp, cache, pages, vp, vp, ci, ci, vp]
+    L.hgf_kv8_gather.restype = ci
+    L.hgf_kv8_gather.argtypes = [cache, pages, vp, vp, ci, ci, vp, vp, vp]
+    L.hgf_diff_attention_kv8_workspace_bytes.restype = sz
+    L.hgf_diff_attention_kv8_workspace_bytes.argtypes = [ci, pages, ci, ci]
+    L.hgf_diff_attention_decode_kv8.restype = ci
+    L.hgf_diff_attention_decode_kv8.argtypes = [vp, cache, pages, vp, ci, cf, cf, vp, vp, vp, sz, vp]
     L.hgf_packed_weight_bytes_b3.restype = sz
     L.hgf_packed_weight_bytes_b3.argtypes = [ci, ci]
     L.hgf_quantize_pack_weights_b3.restype = ci
@@ -336,6 +368,241 @@ def hgf_diff_attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
     _check(lib().hgf_diff_attention_decode(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), lens.data_ptr(), B, L,
                                            H, d_h, float(lam), out.data_ptr(), workspace.data_ptr(),
                                            workspace.numel(), _stream(stream)), "hgf_diff_attention_decode")
+    return out
+
+
+# --------------------------------------------------------------------------- attention over prompts, the paged 8-bit cache
+#
+# These calls take tensors of one device, which is made the current one for the call, and by default that
+# device's current stream.  What they allocate for the caller belongs to the call's stream.
+
+def _at(device, stream):
+    return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+
+
+def _on(device, call, where: str, *args, stream=None) -> None:
+    if stream is not None and stream.device != device:
+        raise ValueError(f"a stream of {stream.device} for tensors of {device}")
+    with torch.cuda.device(device):
+        _check(call(*args, _stream(stream)), where)
+
+
+def _same_device(device, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors of {t.device} and {device} in one call")
+
+
+def _new_ints(device, stream, *shape: int) -> torch.Tensor:
+    with _at(device, stream):
+        return torch.empty(shape, dtype=torch.int32, device=device)
+
+
+def _ints(t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str) -> Optional[torch.Tensor]:
+    if t is not None:
+        _dev(t, torch.int32, name)
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}")
+    return t
+
+
+def _halves(t: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
+    _dev(t, torch.float16, name)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    return t
+
+
+def _slopes(t: Optional[torch.Tensor], n_heads: int) -> Optional[torch.Tensor]:
+    if t is not None:
+        _dev(t, torch.float32, "slopes")
+        if tuple(t.shape) != (2 * n_heads,):
+            raise ValueError("slopes must be [2H]")
+    return t
+
+
+def hgf_diff_attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, lam: float,
+                               cu_k: Optional[torch.Tensor] = None, causal: bool = True,
+                               prefix: Optional[torch.Tensor] = None, doc_q: Optional[torch.Tensor] = None,
+                               doc_k: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                               slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                               stream=None) -> torch.Tensor:
+    """Differential attention of a packed batch of prompts: q fp16 [Tq, 2H, d_h], k [Tk, 2H, d_h], v [Tk, H, d_h],
+    cu_q, cu_k int32 [B + 1] (cu_k None: cu_q) -> fp16 [Tq, H, d_h].  The last query of a sequence stands at its last
+    key.  prefix int32 [B]: keys that every row sees; doc_q, doc_k int32: document numbers (negative: padding);
+    softcap: scores become softcap tanh(score / softcap); slopes fp32 [2H]: minus slope times the distance.  Without
+    `out`, rows that belong to no sequence come back as zero."""
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _dev(t, torch.float16, n)
+    if q.dim() != 3 or v.dim() != 3 or q.shape[1] != 2 * v.shape[1] or q.shape[2] != v.shape[2]:
+        raise ValueError("shapes: q [Tq, 2H, d_h], k [Tk, 2H, d_h], v [Tk, H, d_h]")
+    Tq, H2, d_h = q.shape
+    Tk, H = v.shape[:2]
+    _halves(k, (Tk, H2, d_h), "k")
+    _dev(cu_q, torch.int32, "cu_q")
+    B = cu_q.numel() - 1
+    _ints(cu_q, (B + 1,), "cu_q"), _ints(cu_k, (B + 1,), "cu_k"), _ints(prefix, (B,), "prefix")
+    _ints(doc_q, (Tq,), "doc_q"), _ints(doc_k, (Tk,), "doc_k"), _slopes(slopes, H)
+    if out is None:
+        with _at(q.device, stream):
+            out = torch.zeros((Tq, H, d_h), dtype=torch.float16, device=q.device)
+    _halves(out, (Tq, H, d_h), "out")
+    _same_device(q.device, k, v, cu_q, cu_k, prefix, doc_q, doc_k, slopes, out)
+    _on(q.device, lib().hgf_diff_attention_prefill, "hgf_diff_attention_prefill", q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        cu_q.data_ptr(), _ptr(cu_k), B, Tq, Tk, H, d_h, float(lam), 1 if causal else 0, _ptr(prefix), _ptr(doc_q),
+        _ptr(doc_k), float(softcap), _ptr(slopes), out.data_ptr(), stream=stream)
+    return out
+
+
+class Kv8Pages:
+    """Page table, lengths and reference counts of up to n_seqs sequences, for any number of Kv8Caches."""
+
+    def __init__(self, n_pages: int, page: int, n_seqs: int, max_pages: int, device="cuda"):
+        self.table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        self.n_pages, self.page, self.n_seqs, self.max_pages = n_pages, page, n_seqs, max_pages
+        self.device = self.table.device
+        self.c = hgf_kv8_pages(n_pages, page, n_seqs, max_pages, self.table.data_ptr(), self.lens.data_ptr(),
+                               self.refs.data_ptr())
+
+
+class Kv8Cache:
+    """Pages of codes and scales of one layer's keys and values."""
+
+    def __init__(self, n_pages: int, page: int, n_heads: int, d_h: int, device="cuda"):
+        if d_h not in (16, 32, 64, 128) or page not in (16, 32, 64, 128, 256):
+            raise ValueError("d_h must be 16, 32, 64 or 128, page 16, 32, 64, 128 or 256")
+        blocks = page // 16
+        self.k_codes = torch.zeros((n_pages, 2 * n_heads, blocks, d_h // 16, 16, 16), dtype=torch.int8, device=device)
+        self.v_codes = torch.zeros((n_pages, n_heads, blocks, d_h, 16), dtype=torch.int8, device=device)
+        self.k_scale = torch.zeros((n_pages, 2 * n_heads, blocks), dtype=torch.float32, device=device)
+        self.v_scale = torch.zeros((n_pages, n_heads, blocks), dtype=torch.float32, device=device)
+        self.n_pages, self.page, self.n_heads, self.d_h = n_pages, page, n_heads, d_h
+        self.device = self.k_codes.device
+        self.c = hgf_kv8_cache(n_pages, page, n_heads, d_h, self.k_codes.data_ptr(), self.k_scale.data_ptr(),
+                               self.v_codes.data_ptr(), self.v_scale.data_ptr())
+
+    def load(self, k_codes: torch.Tensor, k_scale: torch.Tensor, v_codes: torch.Tensor, v_scale: torch.Tensor) -> None:
+        """Fills the pool from int8 codes [n_pages, page / 16, heads, 16, d_h] and fp32 scales [n_pages, page / 16, heads]."""
+        N, nb, H, d = self.n_pages, self.page // 16, self.n_heads, self.d_h
+        self.k_codes.copy_(k_codes.view(N, nb, 2 * H, 16, d // 16, 16).permute(0, 2, 1, 4, 3, 5))
+        self.v_codes.copy_(v_codes.permute(0, 2, 1, 4, 3))
+        self.k_scale.copy_(k_scale.transpose(1, 2))
+        self.v_scale.copy_(v_scale.transpose(1, 2))
+
+
+def hgf_kv8_pages_grow(pages: Kv8Pages, seqs: torch.Tensor, new: torch.Tensor, ok: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """Sequences seqs (int32 [n]) become new (int32 [n]) positions longer -> int32 [n]: 1, or 0 where refused."""
+    n = seqs.numel()
+    if ok is None:
+        ok = _new_ints(pages.device, stream, n)
+    _ints(seqs, (n,), "seqs"), _ints(new, (n,), "new"), _ints(ok, (n,), "ok")
+    _same_device(pages.device, seqs, new, ok)
+    _on(pages.device, lib().hgf_kv8_pages_grow, "hgf_kv8_pages_grow", ctypes.byref(pages.c), seqs.data_ptr(), new.data_ptr(),
+        n, ok.data_ptr(), stream=stream)
+    return ok
+
+
+def hgf_kv8_pages_fork(pages: Kv8Pages, src: torch.Tensor, dst: torch.Tensor, pairs: Optional[torch.Tensor] = None,
+                       ok: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The empty sequences dst become what src are -> (pairs of pages to copy in every cache int32 [n, 2], ok int32 [n])."""
+    n = src.numel()
+    pairs = _new_ints(pages.device, stream, n, 2) if pairs is None else pairs
+    ok = _new_ints(pages.device, stream, n) if ok is None else ok
+    _ints(src, (n,), "src"), _ints(dst, (n,), "dst"), _ints(pairs, (n, 2), "pairs"), _ints(ok, (n,), "ok")
+    _same_device(pages.device, src, dst, pairs, ok)
+    _on(pages.device, lib().hgf_kv8_pages_fork, "hgf_kv8_pages_fork", ctypes.byref(pages.c), src.data_ptr(), dst.data_ptr(), n,
+        pairs.data_ptr(), ok.data_ptr(), stream=stream)
+    return pairs, ok
+
+
+def hgf_kv8_pages_free(pages: Kv8Pages, seqs: torch.Tensor, stream=None) -> None:
+    """The sequences become empty; pages that no sequence has any more are free."""
+    n = seqs.numel()
+    _ints(seqs, (n,), "seqs")
+    _same_device(pages.device, seqs)
+    _on(pages.device, lib().hgf_kv8_pages_free, "hgf_kv8_pages_free", ctypes.byref(pages.c), seqs.data_ptr(), n, stream=stream)
+
+
+def hgf_kv8_pages_compact(pages: Kv8Pages, pairs: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                          moved: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The pages in use get the lowest numbers -> (pairs int32 [max(1, n_pages / 2), 2] to copy in every cache, their
+    number int32 [1], the new number of every page int32 [n_pages])."""
+    room = max(1, pages.n_pages // 2)
+    pairs = _new_ints(pages.device, stream, room, 2) if pairs is None else pairs
+    count = _new_ints(pages.device, stream, 1) if count is None else count
+    moved = _new_ints(pages.device, stream, pages.n_pages) if moved is None else moved
+    _ints(pairs, (room, 2), "pairs"), _ints(count, (1,), "count"), _ints(moved, (pages.n_pages,), "moved")
+    _same_device(pages.device, pairs, count, moved)
+    _on(pages.device, lib().hgf_kv8_pages_compact, "hgf_kv8_pages_compact", ctypes.byref(pages.c), pairs.data_ptr(),
+        count.data_ptr(), moved.data_ptr(), stream=stream)
+    return pairs, count, moved
+
+
+def hgf_kv8_copy_pages(cache: Kv8Cache, pairs: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Copies page pairs[i][0] of the cache to page pairs[i][1]; with count (int32 [1]) the first so many."""
+    n = pairs.shape[0]
+    _ints(pairs, (n, 2), "pairs"), _ints(count, (1,), "count")
+    _same_device(cache.device, pairs, count)
+    _on(cache.device, lib().hgf_kv8_copy_pages, "hgf_kv8_copy_pages", ctypes.byref(cache.c), pairs.data_ptr(), _ptr(count), n,
+        stream=stream)
+
+
+def hgf_kv8_append(k: torch.Tensor, v: torch.Tensor, cache: Kv8Cache, pages: Kv8Pages, cu_new: Optional[torch.Tensor] = None,
+                   seqs: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Writes new tokens, k fp16 [T, 2H, d_h] and v [T, H, d_h], as the last positions of their sequences: row b of the batch
+    is sequence seqs[b] (None: b) and has rows cu_new[b] .. cu_new[b+1]-1 (int32 [B + 1]; None: one each)."""
+    T = v.shape[0]
+    _halves(k, (T, 2 * cache.n_heads, cache.d_h), "k"), _halves(v, (T, cache.n_heads, cache.d_h), "v")
+    B = cu_new.numel() - 1 if cu_new is not None else T
+    _ints(cu_new, (B + 1,), "cu_new"), _ints(seqs, (B,), "seqs")
+    _same_device(cache.device, k, v, pages.table, cu_new, seqs)
+    _on(cache.device, lib().hgf_kv8_append, "hgf_kv8_append", k.data_ptr(), v.data_ptr(), ctypes.byref(cache.c),
+        ctypes.byref(pages.c), _ptr(seqs), _ptr(cu_new), B, T, stream=stream)
+
+
+def hgf_kv8_gather(cache: Kv8Cache, pages: Kv8Pages, cu: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   seqs: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The last cu[b+1] - cu[b] positions of row b's sequence as fp16, into rows cu[b] .. of k [T, 2H, d_h] and v [T, H, d_h]."""
+    T = v.shape[0]
+    _halves(k, (T, 2 * cache.n_heads, cache.d_h), "k"), _halves(v, (T, cache.n_heads, cache.d_h), "v")
+    B = cu.numel() - 1
+    _ints(cu, (B + 1,), "cu"), _ints(seqs, (B,), "seqs")
+    _same_device(cache.device, k, v, pages.table, cu, seqs)
+    _on(cache.device, lib().hgf_kv8_gather, "hgf_kv8_gather", ctypes.byref(cache.c), ctypes.byref(pages.c), _ptr(seqs),
+        cu.data_ptr(), B, T, k.data_ptr(), v.data_ptr(), stream=stream)
+    return k, v
+
+
+def hgf_diff_attention_kv8_workspace_bytes(B: int, pages: Kv8Pages, n_heads: int, d_h: int) -> int:
+    return lib().hgf_diff_attention_kv8_workspace_bytes(B, ctypes.byref(pages.c), n_heads, d_h)
+
+
+def hgf_diff_attention_decode_kv8(q: torch.Tensor, cache: Kv8Cache, pages: Kv8Pages, lam: float,
+                                  seqs: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                                  slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                                  workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """One decode step over the 8-bit cache: q fp16 [B, 2H, d_h], row b of sequence seqs[b] (None: b), whose newest token
+    has been appended -> fp16 [B, H, d_h]."""
+    B = q.shape[0]
+    H, d_h = cache.n_heads, cache.d_h
+    _halves(q, (B, 2 * H, d_h), "q")
+    _ints(seqs, (B,), "seqs"), _slopes(slopes, H)
+    need = hgf_diff_attention_kv8_workspace_bytes(B, pages, H, d_h)
+    with _at(cache.device, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if out is None:
+            out = torch.empty((B, H, d_h), dtype=torch.float16, device=q.device)
+    _halves(out, (B, H, d_h), "out")
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor in device memory")
+    _same_device(cache.device, q, pages.table, seqs, slopes, out, workspace)
+    _on(cache.device, lib().hgf_diff_attention_decode_kv8, "hgf_diff_attention_decode_kv8", q.data_ptr(),
+        ctypes.byref(cache.c), ctypes.byref(pages.c), _ptr(seqs), B, float(lam), float(softcap), _ptr(slopes), out.data_ptr(),
+        workspace.data_ptr() if need else None, workspace.numel() * workspace.element_size(), stream=stream)
     return out
 
 
