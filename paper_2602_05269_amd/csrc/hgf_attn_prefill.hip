@@ -2,33 +2,41 @@
 //
 //   out = (softmax(s1) V - lambda softmax(s2) V) / 2, both branches in one pass over the keys with running maxima and sums.
 //
-// A workgroup holds 128 query rows of one head and sequence, a wavefront 32 of them for both branches, and takes the
-// keys 64 at a time: K1, K2 and V of the tile in LDS, double buffered, requested a tile ahead.  All products are
-// computed transposed, S^T = K Q^T and O^T = V^T P^T on the 32x32x16 fp16 matrix instruction, so that a lane
-// owns one query: its maximum, sum and rescaling are registers of the lane (one exchange between the halves of the wavefront),
-// and the 8 weights of a step that a lane holds after S^T are the ones it has to supply for O^T if V's keys are taken in
-// the order in which the accumulator's rows lie (4 h .. 4 h + 3 and 8 + 4 h .. for half h): P never moves.  V is
-// transposed on its way into LDS.
+// A workgroup of eight wavefronts holds 128 query rows of one head and sequence, a wavefront 32 of them for one of the branches, and
+// takes the keys 64 at a time: K1, K2 and V of the tile in LDS, double buffered, requested a tile ahead.  All
+// products are computed transposed, S^T = K Q^T and O^T = V^T P^T on the 32x32x16 fp16 matrix instruction, so that
+// a lane owns one query: its maximum, sum and rescaling are registers of the lane (one exchange between the halves of the
+// wavefront), and the 8 weights of a step that a lane holds after S^T are the ones it has to supply for O^T if V's
+// keys are taken in the order in which the accumulator's rows lie (4 h .. 4 h + 3 and 8 + 4 h .. for half h): P never
+// moves.  V is transposed on its way into LDS.
+// Few rows would leave most of the chip idle: then (SPLIT) a workgroup holds 32 rows, takes 128 keys at a time, and its
+// wavefronts share the keys of a tile; they are merged at the end.
 // Weights are relative to the running maximum in base 2 and carried 2^7 larger, so that fp16 holds them down to
-// 2^-31; the maximum is only raised when a tile exceeds it by 2^8 (which the factor leaves room for), which spares
+// 2^-31; a row's maximum is only raised when a tile exceeds it by 2^8 (which the factor leaves room for), which spares
 // most rescalings.  fp32: scores, weights before rounding, sums, outputs.  The sum adds up the rounded weights.
 // Masks are one comparison per element, key < limit of the row, and a comparison of document numbers where documents are
-// given, both only in tiles that need them.  What a row does not see has weight 0; values of V that
-// are no finite numbers are taken out of the tile and added to the rows that see them (0 * inf would reach
-// the others).
-// Bound by the exponentials and the vector instructions around them: 64 scores per lane and tile against
-// 32 matrix instructions (64 columns).
+// given, both only in tiles that need them; tiles whose document numbers lie outside those of the rows are not
+// read.  What a row does not see has weight 0; values of V that are no finite numbers are taken out of the tile and
+// added to the rows that see them (0 * inf would reach the others).
+// Bound by the exponentials and the vector instructions around them up to 64 columns: 32 scores per lane and
+// tile against 16 matrix instructions.
 #include "hgf_kv8.h"
 
+#include <limits.h>
 #include <type_traits>
 
 namespace hgf {
 
 namespace {
 
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kRows = 128, kKeys = 64;
+constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr float kLift = 7.0f, kSlack = 8.0f;
+// From here on 1 - 2 / (e^2y + 1) is too coarse a tanh near 0: its error, 2^-23 of the cap, passes 6e-5.
+constexpr float kCoarseCap = 512.0f;
 
 struct PrefillParams {
     PrefillArgs a;
@@ -36,53 +44,66 @@ struct PrefillParams {
     int slots;
 };
 
-__device__ inline float soft_cap(float x, float cap, float inv)
-{
-    const float y = x * inv, y2 = y * y;
-    const float series = y * __builtin_fmaf(y2, __builtin_fmaf(y2, __builtin_fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-    const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * kLog2e)) + 1.0f);
-    return cap * (fabsf(y) < 0.3f ? series : t);
-}
-
-// Position of a 16-byte chunk of row `row` in LDS, so that the eight rows that are read together lie in different banks.
-template <int D>
-__device__ inline int k_chunk(int row, int c)
-{
-    constexpr int C = D / 8;                        // chunks of a row
-    return row * C + (C >= 8 ? c ^ (row & 7) : C == 4 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1));
-}
-__device__ inline int v_chunk(int d, int c) { return d * (kKeys / 8) + (c ^ ((d ^ (d >> 3)) & 7)); }
-
-template <int D>
-struct Tile {
-    static constexpr int kK = kKeys * D, kV = (D < 32 ? 32 : D) * kKeys;        // halves
-    static constexpr int kHalves = 2 * kK + kV;
+// Sizes of one variant.
+template <int D, int SPLIT>
+struct Shape {
+    static constexpr int kRows = 128 / SPLIT, kKeys = SPLIT == 1 ? 64 : 128;
+    static constexpr int kSub = kKeys / 32 / SPLIT;             // groups of 32 keys per wavefront and tile
+    static constexpr int kChunksK = D / 8, kChunksV = kKeys / 8;
+    static constexpr int kK = kKeys * D, kV = (D < 32 ? 32 : D) * kKeys, kHalves = 2 * kK + kV;
+    static constexpr int kBufs = 2 * kHalves * 2 <= 147456 ? 2 : 1;
+    static constexpr int kTileT = (D + 31) / 32;                // row tiles of O^T
+    // outputs on their way between wavefronts, in the tiles' place
+    static constexpr size_t kLds = (size_t)kBufs * kHalves * 2;
+    static_assert((size_t)(SPLIT == 1 ? 4 : 6) * kTileT * 4096 <= kLds, "the merge fits where the tiles were");
 };
 
-template <int D, bool MOD>
-__global__ __launch_bounds__(256) void prefill_attn_kernel(PrefillParams p)
+// Place of a 16-byte chunk of row `row` of K, and of column d of V, so that the eight rows that are read together lie in
+// different banks.
+template <int C>
+__device__ inline int k_chunk(int row, int c)
 {
-    constexpr int KS = D / 16, DT = (D + 31) / 32;  // steps of S^T; row tiles of O^T
-    constexpr int KP = kKeys * D / 8 / 256 > 0 ? kKeys * D / 8 / 256 : 1;       // 16-byte pieces of a K per thread (D = 16: half the threads)
-    constexpr int VT = kKeys * D / 16;              // 4 x 4 pieces of V of a tile
-    constexpr int VP = VT / 256 > 0 ? VT / 256 : 1;
+    return row * C + (C >= 8 ? c ^ (row & 7) : C == 4 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1));
+}
+template <int C>
+__device__ inline int v_chunk(int d, int c) { return d * C + (c ^ ((d ^ (d >> 3)) & 7)); }
+
+// A value that the compiler does not see through: what rare paths compute from it is computed there, instead of being kept
+// in registers across the loop.
+__device__ inline int opaque(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ inline float halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+
+template <int D, bool MOD, int SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams p)
+{
+    using S = Shape<D, SPLIT>;
+    constexpr int KS = D / 16, DT = S::kTileT, SUB = S::kSub, CK = S::kChunksK, CV = S::kChunksV;
+    constexpr int KP = 2 * S::kKeys * CK / kThreads > 0 ? 2 * S::kKeys * CK / kThreads : 1;     // 16-byte pieces of K per thread
+    constexpr int KALL = 2 * S::kKeys * CK;
+    constexpr int VALL = S::kKeys * D / 16, VP = VALL > kThreads ? VALL / kThreads : 1;         // 4 x 4 pieces of V per thread
     extern __shared__ __align__(16) _Float16 lds[];
-    __shared__ int odd_s[2][4];
-    __shared__ int doc_s[2][kKeys];
+    __shared__ int odd_s[2][kWaves], doc_s[2][S::kKeys];
+    __shared__ int most_s[kWaves], lo_s[kWaves], hi_s[kWaves], win_lo[kWaves][64], win_hi[kWaves][64];
+    __shared__ float m_s[SPLIT][2][32], sum_s[SPLIT][2][32];
     const PrefillArgs &a = p.a;
     const int H = a.n_heads, h = blockIdx.x % H;
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = l >> 5, col = l & 31;
+    const int br = w >> 2, group = SPLIT == 1 ? w & 3 : 0, split = SPLIT == 1 ? 0 : w & 3;
 
-    // ---- which rows: the slots of sequence b begin at cu_q[b] / 128 + b; the last ones first (they see the most keys)
+    // ---- which rows: the slots of sequence b begin at cu_q[b] / kRows + b; the last ones first (they see the most keys)
     const int slot = p.slots - 1 - (int)(blockIdx.x / H);
-    const int b = wave_search(a.B, slot, [&](int x) { return min(max(a.cu_q[x], 0), a.Tq) / kRows + x; });
+    const int b = wave_search(a.B, slot, [&](int x) { return min(max(a.cu_q[x], 0), a.Tq) / S::kRows + x; });
     int q0, nq, k0, nk;
     clipped_rows(a.cu_q, b, a.Tq, q0, nq);
     clipped_rows(a.cu_k, b, a.Tk, k0, nk);
-    const int first = (slot - q0 / kRows - b) * kRows;
+    const int first = (slot - q0 / S::kRows - b) * S::kRows;
     if (first < 0 || first >= nq) return;
-    const int row = first + w * 32 + col;           // the lane's query
+    const int row = first + group * 32 + col;       // the lane's query
     const bool real = row < nq;
     const int pos = nk - nq + row;                  // its position among the keys
     int limit = a.causal ? max(pos + 1, a.prefix ? a.prefix[b] : 0) : nk;       // it sees keys below
@@ -93,74 +114,88 @@ __global__ __launch_bounds__(256) void prefill_attn_kernel(PrefillParams p)
         if (doc < 0) limit = 0;
     }
     if (!real) limit = 0;
-    // rows of the wavefront that see the fewest and the most (missing rows do not count as seeing few)
-    const int least = -(int)wave_max((float)-(real && doc >= 0 ? limit : nk)), most = (int)wave_max((float)limit);
-    __shared__ int most_s[4];
-    if (l == 0) most_s[w] = most;
-    __syncthreads();
-    const int end = max(max(most_s[0], most_s[1]), max(most_s[2], most_s[3]));
-    const int tiles = (end + kKeys - 1) / kKeys;
+    const bool counts = real && doc >= 0;
+    // the fewest keys that a row of the wavefront sees (0 for padding: its rows see none), and the most
+    const int least = -(int)wave_max((float)-(real ? limit : nk)), most = (int)wave_max((float)limit);
+    int tiles, doc_lo = 0, doc_hi = 0;
+    {
+        int lo = counts ? doc : INT_MAX, hi = counts ? doc : -1;
+        if (a.doc_q) {
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                lo = min(lo, __shfl_xor(lo, o, 64));
+                hi = max(hi, __shfl_xor(hi, o, 64));
+            }
+        }
+        if (l == 0) {
+            most_s[w] = most;
+            lo_s[w] = lo;
+            hi_s[w] = hi;
+        }
+        __syncthreads();
+        int end = 0;
+        doc_lo = INT_MAX;
+        doc_hi = -1;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            end = max(end, most_s[i]);
+            doc_lo = min(doc_lo, lo_s[i]);
+            doc_hi = max(doc_hi, hi_s[i]);
+        }
+        tiles = __builtin_amdgcn_readfirstlane((end + S::kKeys - 1) / S::kKeys);
+    }
 
     // ---- the queries, operand B of S^T
-    v8h q[2][KS];
+    v8h q[KS];
     {
-        const size_t at = ((size_t)(q0 + min(row, nq - 1)) * 2 * H + h) * D + half * 8;
+        const _Float16 *src = a.q + ((size_t)(q0 + min(row, nq - 1)) * 2 * H + br * H + h) * D + half * 8;
 #pragma unroll
-        for (int br = 0; br < 2; ++br)
-#pragma unroll
-            for (int s = 0; s < KS; ++s) q[br][s] = *reinterpret_cast<const v8h *>(a.q + at + (size_t)br * H * D + s * 16);
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h *>(src + s * 16);
     }
-    const float cap = a.softcap, cap_inv = cap > 0.0f ? 1.0f / cap : 0.0f;
-    float slope[2] = {0.0f, 0.0f};
-    if (MOD && a.slopes) {
-        slope[0] = a.slopes[h] * kLog2e;
-        slope[1] = a.slopes[H + h] * kLog2e;
-    }
-    const float unit = MOD ? p.scale : p.scale * kLog2e;
+    const float cap = a.softcap;
+    float slope = 0.0f;
+    if (MOD && a.slopes) slope = a.slopes[br * H + h] * kLog2e;
+    const float unit = MOD ? 1.0f : p.scale * kLog2e;
+    const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};
 
-    v4u kr[2][KP];
+    v4u kr[KP];
     uint2 vr[VP][4];
     int doc_r = 0;
     auto request = [&](int tile) {
-        const int key0 = tile * kKeys;
+        const int key0 = tile * S::kKeys;
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
-            const int at = i * 256 + tid, key = min(key0 + at / (D / 8), nk - 1), c = at % (D / 8);
-            if (D >= 32 || tid < kKeys * D / 8) {
-#pragma unroll
-                for (int br = 0; br < 2; ++br)
-                    kr[br][i] = *reinterpret_cast<const v4u *>(a.k + ((size_t)(k0 + key) * 2 * H + br * H + h) * D + c * 8);
-            }
+            const int at = i * kThreads + tid, kb = at / (KALL / 2), in = at % (KALL / 2);
+            const int key = min(key0 + in / CK, nk - 1), c = in % CK;
+            if (KALL >= kThreads || tid < KALL)
+                kr[i] = *reinterpret_cast<const v4u *>(a.k + ((size_t)(k0 + key) * 2 * H + kb * H + h) * D + c * 8);
         }
 #pragma unroll
         for (int i = 0; i < VP; ++i) {
-            const int at = i * 256 + tid, key = key0 + at / (D / 4) * 4, c = at % (D / 4);
-            if (VT >= 256 || tid < VT) {
+            const int at = i * kThreads + tid, key = key0 + at / (D / 4) * 4, c = at % (D / 4);
+            if (VALL >= kThreads || tid < VALL) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     vr[i][j] = *reinterpret_cast<const uint2 *>(a.v + ((size_t)(k0 + min(key + j, nk - 1)) * H + h) * D + c * 4);
             }
         }
-        if (a.doc_k && tid < kKeys) doc_r = key0 + tid < nk ? a.doc_k[k0 + key0 + tid] : -1;
+        if (a.doc_k && tid < S::kKeys) doc_r = key0 + tid < nk ? a.doc_k[k0 + key0 + tid] : -1;
     };
-    // Into LDS; V as columns of 64 keys, the keys of a step of 16 in the order 0-3, 8-11, 4-7, 12-15.
+    // Into LDS; V as columns of keys, the keys of a step of 16 in the order 0-3, 8-11, 4-7, 12-15.
     auto deposit = [&](int buf) {
-        _Float16 *kb = lds + buf * Tile<D>::kHalves, *vb = kb + 2 * Tile<D>::kK;
+        _Float16 *kb = lds + buf * S::kHalves, *vb = kb + 2 * S::kK;
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
-            const int at = i * 256 + tid;
-            if (D >= 32 || tid < kKeys * D / 8) {
-#pragma unroll
-                for (int br = 0; br < 2; ++br)
-                    reinterpret_cast<v4u *>(kb + br * Tile<D>::kK)[k_chunk<D>(at / (D / 8), at % (D / 8))] = kr[br][i];
-            }
+            const int at = i * kThreads + tid;
+            if (KALL >= kThreads || tid < KALL)
+                reinterpret_cast<v4u *>(kb + at / (KALL / 2) * S::kK)[k_chunk<CK>(at % (KALL / 2) / CK, at % CK)] = kr[i];
         }
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < VP; ++i) {
-            const int at = i * 256 + tid, quad = at / (D / 4), c = at % (D / 4);
-            if (VT >= 256 || tid < VT) {
-                const int slot8 = (quad & ~3) + ((quad & 1) << 1 | (quad & 2) >> 1);    // 8-byte place in a column
+            const int at = i * kThreads + tid, quad = at / (D / 4), c = at % (D / 4);
+            if (VALL >= kThreads || tid < VALL) {
+                const int place = (quad & ~3) + ((quad & 1) << 1 | (quad & 2) >> 1);    // 8-byte place in a column
                 uint32_t o = 0;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -185,144 +220,249 @@ __global__ __launch_bounds__(256) void prefill_attn_kernel(PrefillParams p)
                     const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
                     auto word = [&](int j) { return e < 2 ? vr[i][j].x : vr[i][j].y; };
                     const uint2 x = make_uint2(__builtin_amdgcn_perm(word(1), word(0), sel), __builtin_amdgcn_perm(word(3), word(2), sel));
-                    const int chunk = v_chunk(c * 4 + e, slot8 >> 1);
-                    *reinterpret_cast<uint2 *>(vb + chunk * 8 + (slot8 & 1) * 4) = x;
+                    *reinterpret_cast<uint2 *>(vb + v_chunk<CV>(c * 4 + e, place >> 1) * 8 + (place & 1) * 4) = x;
                 }
             }
         }
-        if (a.doc_k && tid < kKeys) doc_s[buf][tid] = doc_r;
+        if (a.doc_k && tid < S::kKeys) doc_s[buf][tid] = doc_r;
         const bool any = __any(odd);
         if (l == 0) odd_s[buf][w] = any ? 1 : 0;
     };
 
-    float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
-    v16f o[2][DT];
+    float m = -INFINITY, sum = 0.0f;
+    v16f o[DT];
 #pragma unroll
-    for (int br = 0; br < 2; ++br)
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[br][t][e] = 0.0f;
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
 
-    if (tiles > 0) {
-        request(0);
-        deposit(0);
-    }
-    __syncthreads();
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int buf = tile & 1, key0 = tile * kKeys;
-        if (tile + 1 < tiles) request(tile + 1);
-        if (key0 < most) {
-            const _Float16 *kb = lds + buf * Tile<D>::kHalves, *vb = kb + 2 * Tile<D>::kK;
-            const bool partial = key0 + kKeys > least || a.doc_k;
-            v8h pr[2][4];                           // weights of both branches, operand B of O^T
+    // `same`: every key of the tile has the one document of all the rows
+    auto compute = [&](int tile, int buf, bool same) {
+        const int sub0 = split * SUB, key0 = tile * S::kKeys + sub0 * 32;           // the wavefront's keys of the tile
+        if (key0 >= most) return;
+        const _Float16 *kb = lds + buf * S::kHalves + br * S::kK, *vb = lds + buf * S::kHalves + 2 * S::kK;
+        const bool docs = a.doc_k && !same;
+        v16f s[SUB];
 #pragma unroll
-            for (int br = 0; br < 2; ++br) {
-                v16f s[2];
+        for (int kt = 0; kt < SUB; ++kt) {
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
+            for (int e = 0; e < 16; ++e) s[kt][e] = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[kt][e] = 0.0f;
-#pragma unroll
-                    for (int st = 0; st < KS; ++st) {
-                        const v8h x = *reinterpret_cast<const v8h *>(kb + br * Tile<D>::kK + k_chunk<D>(kt * 32 + col, st * 2 + half) * 8);
-                        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[br][st], s[kt], 0, 0, 0);
-                    }
-                }
-                // scores in base 2
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float x = s[kt][e] * unit;
-                        if (MOD) {
-                            const int key = key0 + kt * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                            if (cap > 0.0f) x = soft_cap(x, cap, cap_inv);
-                            x = x * kLog2e - slope[br] * fabsf((float)(pos - key));
-                        }
-                        s[kt][e] = x;
-                    }
-                if (partial) {
-#pragma unroll
-                    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int in = kt * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                            bool seen = key0 + in < limit;
-                            if (a.doc_k) seen = seen && doc_s[buf][in] == doc;
-                            s[kt][e] = seen ? s[kt][e] : -INFINITY;
-                        }
-                }
-                float top = s[0][0];
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kt][e]);
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const bool raise = top > m[br] + kSlack;            // (for each row by itself: no row depends on its neighbours)
-                if (__any(raise)) {
-                    const float next = raise ? top : m[br];
-                    const float corr = __builtin_amdgcn_exp2f(m[br] - (next == -INFINITY ? 0.0f : next));
-                    m[br] = next;
-                    sum[br] *= corr;
-#pragma unroll
-                    for (int t = 0; t < DT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[br][t][e] *= corr;
-                }
-                const float base = (m[br] == -INFINITY ? 0.0f : m[br]) - kLift;
-                float add = 0.0f;
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const _Float16 x = (_Float16)__builtin_amdgcn_exp2f(s[kt][e] - base);
-                        pr[br][kt * 2 + (e >> 3)][e & 7] = x;
-                        add += (float)x;
-                    }
-                sum[br] += add;
+            for (int st = 0; st < KS; ++st) {
+                const v8h x = *reinterpret_cast<const v8h *>(kb + k_chunk<CK>((sub0 + kt) * 32 + col, st * 2 + half) * 8);
+                s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[st], s[kt], 0, 0, 0);
             }
+        }
+        // in base 2 from here on: s * unit
+        if (MOD) {
+            if (cap > 0.0f) {
+                const float in = p.scale / cap, out = cap * kLog2e;
+#pragma unroll
+                for (int kt = 0; kt < SUB; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float y = s[kt][e] * in;
+                        const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * kLog2e)) + 1.0f);
+                        if (cap > kCoarseCap) {
+                            const float y2 = y * y;
+                            const float series = y * __builtin_fmaf(y2, __builtin_fmaf(y2, __builtin_fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f),
+                                                                                     -1.0f / 3.0f), 1.0f);
+                            s[kt][e] = (fabsf(y) < 0.3f ? series : t) * out;
+                        } else {
+                            s[kt][e] = t * out;
+                        }
+                    }
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < SUB; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[kt][e] *= p.scale * kLog2e;
+            }
+            if (a.slopes) {
+                const float away = (float)(pos - key0 - 4 * half);
+#pragma unroll
+                for (int kt = 0; kt < SUB; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        s[kt][e] = __builtin_fmaf(-slope, fabsf(away - (float)(kt * 32 + 8 * (e >> 2) + (e & 3))), s[kt][e]);
+            }
+        }
+        if (docs) {
+            const int left = opaque(limit - key0 - 4 * half);
+            const v4i *ids = reinterpret_cast<const v4i *>(doc_s[buf] + sub0 * 32 + opaque(4 * half));
+#pragma unroll
+            for (int kt = 0; kt < SUB; ++kt)
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const v4i id = ids[kt * 8 + e4 * 2];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[kt][e4 * 4 + e] = kt * 32 + 8 * e4 + e < left && id[e] == doc ? s[kt][e4 * 4 + e] : -INFINITY;
+                }
+        } else if (key0 + SUB * 32 > least) {
+            const int left = opaque(limit - key0 - 4 * half);
+#pragma unroll
+            for (int kt = 0; kt < SUB; ++kt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[kt][e] = kt * 32 + 8 * (e >> 2) + (e & 3) < left ? s[kt][e] : -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int kt = 0; kt < SUB; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[kt][e]), s[kt][e + 1]);
+        top = halves_max(top) * unit;
+        const bool raise = top > m + kSlack;            // (for each row by itself: no row depends on its neighbours)
+        if (__any(raise)) {
+            const float next = raise ? top : m;
+            const float corr = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next));
+            m = next;
+            sum *= corr;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const v8h x = *reinterpret_cast<const v8h *>(vb + v_chunk(t * 32 + col, st * 2 + half) * 8);
+                for (int e = 0; e < 16; ++e) o[t][e] *= corr;
+        }
+        const float base = kLift - (m == -INFINITY ? 0.0f : m);
+        v8h pr[SUB * 2];                                // the weights, operand B of O^T
 #pragma unroll
-                    for (int br = 0; br < 2; ++br) o[br][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pr[br][st], o[br][t], 0, 0, 0);
-                }
-            if (odd_s[buf][0] | odd_s[buf][1] | odd_s[buf][2] | odd_s[buf][3]) {
-                // values that are no finite numbers, to the rows that see them
-                const int n = min(kKeys, nk - key0);
-                for (int j = 0; j < n; ++j) {
-                    bool seen = key0 + j < limit;
-                    if (a.doc_k) seen = seen && doc_s[buf][j] == doc;
-                    if (!__any(seen)) continue;
-                    const _Float16 *v = a.v + ((size_t)(k0 + key0 + j) * H + h) * D;
+        for (int kt = 0; kt < SUB; ++kt)
 #pragma unroll
-                    for (int t = 0; t < DT; ++t)
+            for (int e = 0; e < 16; e += 2) {
+                v2f x;
+                x[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e], unit, base));
+                x[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e + 1], unit, base));
+                const v2h y = __builtin_convertvector(x, v2h);
+                sum = __builtin_amdgcn_fdot2(y, ones, sum, false);
+                pr[kt * 2 + (e >> 3)][e & 7] = y[0];
+                pr[kt * 2 + (e >> 3)][(e & 7) + 1] = y[1];
+            }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int d = t * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                            const float x = (float)v[d < D ? d : 0];
-                            if (seen && !(fabsf(x) <= 65504.0f)) {
-                                o[0][t][e] += x;
-                                o[1][t][e] += x;
-                            }
-                        }
-                }
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int st = 0; st < SUB * 2; ++st) {
+                const v8h x = *reinterpret_cast<const v8h *>(vb + v_chunk<CV>(t * 32 + col, (sub0 * 2 + st) * 2 + half) * 8);
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pr[st], o[t], 0, 0, 0);
+            }
+        int odd = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) odd |= odd_s[buf][i];
+        if (__builtin_amdgcn_readfirstlane(odd)) {
+            // values that are no finite numbers, to the rows that see them
+            const int n = min(SUB * 32, nk - key0);
+            for (int j = 0; j < n; ++j) {
+                bool seen = key0 + j < limit;
+                if (a.doc_k) seen = seen && doc_s[buf][sub0 * 32 + j] == doc;
+                if (!__any(seen)) continue;
+                const _Float16 *v = a.v + ((size_t)(k0 + key0 + j) * H + h) * D + opaque(4 * half);
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int d = t * 32 + 8 * (e >> 2) + (e & 3);
+                        if (d >= D) continue;                       // (16 columns: rows of O^T that nobody stores)
+                        const float x = (float)v[d];
+                        if (seen && !(fabsf(x) <= 65504.0f)) o[t][e] += x;
+                    }
             }
         }
-        if (tile + 1 < tiles) deposit(buf ^ 1);
+    };
+
+    // ---- the keys, in windows: all of them, or 64 tiles at a time of which those are taken whose documents can matter
+    for (int from = 0; from < tiles; from += 64) {
+        unsigned long long visit = 0, same = 0;
+        int tile = 0;
+        if (a.doc_k) {
+            constexpr int EACH = S::kKeys / kWaves;     // a lane looks at so many keys of tile from + l
+            int lo = INT_MAX, hi = INT_MIN;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int id = a.doc_k[k0 + min((from + l) * S::kKeys + w * EACH + j, nk - 1)];
+                lo = min(lo, id);
+                hi = max(hi, id);
+            }
+            win_lo[w][l] = lo;
+            win_hi[w][l] = hi;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                lo = min(lo, win_lo[i][l]);
+                hi = max(hi, win_hi[i][l]);
+            }
+            visit = __ballot(from + l < tiles && hi >= doc_lo && lo <= doc_hi);
+            same = __ballot(lo == hi && lo == doc_lo && lo == doc_hi);
+            if (visit) tile = from + __builtin_ctzll(visit);
+            __syncthreads();                            // (the window's arrays are read before the next window's are written)
+            if (!visit) continue;
+        }
+        request(tile);
+        deposit(0);
+        __syncthreads();
+        int buf = 0;
+        while (tile < tiles) {
+            int next = tile + 1;
+            bool one = false;
+            if (a.doc_k) {
+                one = (same >> (tile - from)) & 1;
+                visit &= visit - 1;
+                next = visit ? from + __builtin_ctzll(visit) : tiles;
+            }
+            if (next < tiles) request(next);
+            compute(tile, buf, one);
+            if (S::kBufs == 1) __syncthreads();
+            if (S::kBufs == 2) buf ^= 1;
+            if (next < tiles) deposit(buf);
+            __syncthreads();
+            tile = next;
+        }
+        if (!a.doc_k) break;
+    }
+
+    // ---- merge: the wavefronts that shared keys, then the branches
+    sum += __shfl_xor(sum, 32, 64);
+    float *xchg = reinterpret_cast<float *>(lds);
+    auto place = [&](int i, int t, int e) { return ((i * DT + t) * 16 + e) * 64 + l; };
+    if (SPLIT > 1) {
+        if (l < 32) {
+            m_s[split][br][col] = m;
+            sum_s[split][br][col] = sum;
+        }
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < SPLIT; ++i) top = fmaxf(top, m_s[i][br][col]);
+        top = top == -INFINITY ? 0.0f : top;
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SPLIT; ++i) sum += sum_s[i][br][col] * __builtin_amdgcn_exp2f(m_s[i][br][col] - top);
+        const float f = __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                o[t][e] *= f;
+                if (split > 0) xchg[place((split - 1) * 2 + br, t, e)] = o[t][e];
+            }
+        __syncthreads();
+        if (split == 0) {
+#pragma unroll
+            for (int i = 0; i < SPLIT - 1; ++i)
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[t][e] += xchg[place(i * 2 + br, t, e)];
+        }
         __syncthreads();
     }
-    if (!real) return;
-    float f[2];
+    const float f = (sum == 0.0f ? 0.0f : 0.5f / sum) * (br ? a.lambda : 1.0f);
+    if (br == 1 && split == 0) {
 #pragma unroll
-    for (int br = 0; br < 2; ++br) {
-        const float total = sum[br] + __shfl_xor(sum[br], 32, 64);
-        f[br] = total == 0.0f ? 0.0f : 0.5f / total;
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) xchg[place(group, t, e)] = o[t][e] * f;
     }
-    f[1] *= a.lambda;
+    __syncthreads();
+    if (br == 1 || split > 0 || !real) return;
     _Float16 *out = a.out + ((size_t)(q0 + row) * H + h) * D;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -331,7 +471,7 @@ __global__ __launch_bounds__(256) void prefill_attn_kernel(PrefillParams p)
             const int d = t * 32 + 8 * e4 + 4 * half;
             v4h x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = (_Float16)(o[0][t][e4 * 4 + e] * f[0] - o[1][t][e4 * 4 + e] * f[1]);
+            for (int e = 0; e < 4; ++e) x[e] = (_Float16)(o[t][e4 * 4 + e] * f - xchg[place(group, t, e4 * 4 + e)]);
             if (d < D) *reinterpret_cast<v4h *>(out + d) = x;
         }
 }
@@ -343,21 +483,27 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
     PrefillParams p;
     p.a = a;
     p.scale = 1.0f / sqrtf((float)d_h);
-    p.slots = a.Tq / kRows + a.B;
     const bool mod = a.softcap > 0.0f || a.slopes;
+    // fewer workgroups of 128 rows than the chip holds at a time: 32 rows each
+    const bool few = (long long)(a.Tq / 128 + a.B) * a.n_heads < 512;
     hipError_t e = hipSuccess;
-    auto go = [&](auto d, auto m) {
-        constexpr int D = decltype(d)::value;
+    auto go = [&](auto d, auto m, auto split) {
+        constexpr int D = decltype(d)::value, SPLIT = decltype(split)::value;
         constexpr bool MOD = decltype(m)::value;
-        constexpr size_t bytes = 2 * Tile<D>::kHalves * sizeof(_Float16);
+        using S = Shape<D, SPLIT>;
         static OncePerDevice once;
-        e = allow_lds(once, (const void *)(prefill_attn_kernel<D, MOD>), bytes);
+        e = allow_lds(once, (const void *)(prefill_attn_kernel<D, MOD, SPLIT>), S::kLds);
+        p.slots = a.Tq / S::kRows + a.B;
         if (e == hipSuccess)
-            hipLaunchKernelGGL((prefill_attn_kernel<D, MOD>), dim3((unsigned)p.slots * a.n_heads), dim3(256), bytes, st, p);
+            hipLaunchKernelGGL((prefill_attn_kernel<D, MOD, SPLIT>), dim3((unsigned)p.slots * a.n_heads), dim3(kThreads), S::kLds, st, p);
+    };
+    auto variant = [&](auto d, auto m) {
+        if (few) go(d, m, std::integral_constant<int, 4>{});
+        else go(d, m, std::integral_constant<int, 1>{});
     };
     auto both = [&](auto d) {
-        if (mod) go(d, std::true_type{});
-        else go(d, std::false_type{});
+        if (mod) variant(d, std::true_type{});
+        else variant(d, std::false_type{});
     };
     switch (d_h) {
         case 16: both(std::integral_constant<int, 16>{}); break;

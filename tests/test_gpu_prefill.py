@@ -67,6 +67,10 @@ def test_documents():
         _check(q, k, v, cu, doc_q=docs, doc_k=docs, causal=False)
     out = _check(q, k, v, cu, doc_q=padded, doc_k=padded)
     assert not out[61:200].any() and not out[n:].any()
+    # one document and padding among the same 32 rows
+    ends = [0] * 180 + [-1] * 20
+    out = _check(q[:200], k[:200], v[:200], [0, 200], doc_q=ends, doc_k=ends)
+    assert not out[180:].any()
     # documents of the queries that no key has
     _check(q, k, v, cu, doc_q=[9] * (n + 40), doc_k=rising)
 
