@@ -75,7 +75,12 @@ __device__ inline int opaque(int v)
     asm volatile("" : "+v"(v));
     return v;
 }
-__device__ inline float halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+// The larger of a lane's value and of the lane 32 further on or back.
+__device__ inline float halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
 
 template <int D, bool MOD, int SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams p)
@@ -87,7 +92,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     constexpr int VALL = S::kKeys * D / 16, VP = VALL > kThreads ? VALL / kThreads : 1;         // 4 x 4 pieces of V per thread
     extern __shared__ __align__(16) _Float16 lds[];
     __shared__ int odd_s[2][kWaves], doc_s[2][S::kKeys];
-    __shared__ int most_s[kWaves], lo_s[kWaves], hi_s[kWaves], win_lo[kWaves][64], win_hi[kWaves][64];
+    __shared__ int most_s[kWaves], least_s[kWaves], lo_s[kWaves], hi_s[kWaves], win_lo[kWaves][64], win_hi[kWaves][64];
     __shared__ float m_s[SPLIT][2][32], sum_s[SPLIT][2][32];
     const PrefillArgs &a = p.a;
     const int H = a.n_heads, h = blockIdx.x % H;
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     const bool counts = real && doc >= 0;
     // the fewest keys that a row of the wavefront sees (0 for padding: its rows see none), and the most
     const int least = -(int)wave_max((float)-(real ? limit : nk)), most = (int)wave_max((float)limit);
-    int tiles, doc_lo = 0, doc_hi = 0;
+    int tiles, whole, doc_lo = 0, doc_hi = 0;       // tiles that some row sees, that all rows see whole
     {
         int lo = counts ? doc : INT_MAX, hi = counts ? doc : -1;
         if (a.doc_q) {
@@ -129,20 +134,23 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         }
         if (l == 0) {
             most_s[w] = most;
+            least_s[w] = least;
             lo_s[w] = lo;
             hi_s[w] = hi;
         }
         __syncthreads();
-        int end = 0;
+        int end = 0, all = INT_MAX;
         doc_lo = INT_MAX;
         doc_hi = -1;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) {
             end = max(end, most_s[i]);
+            all = min(all, least_s[i]);
             doc_lo = min(doc_lo, lo_s[i]);
             doc_hi = max(doc_hi, hi_s[i]);
         }
         tiles = __builtin_amdgcn_readfirstlane((end + S::kKeys - 1) / S::kKeys);
+        whole = min(tiles, __builtin_amdgcn_readfirstlane(all / S::kKeys));
     }
 
     // ---- the queries, operand B of S^T
@@ -158,51 +166,72 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     const float unit = MOD ? 1.0f : p.scale * kLog2e;
     const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};
 
+    // ---- tiles on their way: global memory -> registers -> LDS.
+    // A tile's rows are read through a descriptor that ends where the sequence does: rows behind it are zeros, and what a
+    // thread adds to the tile's address does not change from tile to tile.
+    const unsigned k_row = (unsigned)H * D * 4, v_row = (unsigned)H * D * 2;
+    auto rows_of = [&](const _Float16 *base, unsigned row_bytes, int key0) {
+        return make_rsrc(reinterpret_cast<const char *>(base) + (size_t)(k0 + key0) * row_bytes, (unsigned)min(nk - key0, S::kKeys) * row_bytes);
+    };
     v4u kr[KP];
     uint2 vr[VP][4];
     int doc_r = 0;
-    auto request = [&](int tile) {
-        const int key0 = tile * S::kKeys;
+    const unsigned k_off = (unsigned)(tid % (KALL / 2) / CK) * k_row + (unsigned)((tid / (KALL / 2) * H + h) * D + tid % CK * 8) * 2;
+    const unsigned v_off = (unsigned)(tid / (D / 4) * 4) * v_row + (unsigned)(h * D + tid % (D / 4) * 4) * 2;
+    auto request_k = [&](int tile) {
+        const rsrc_t r = rows_of(a.k, k_row, tile * S::kKeys);
+        if (KALL >= kThreads || tid < KALL) {
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            const int at = i * kThreads + tid, kb = at / (KALL / 2), in = at % (KALL / 2);
-            const int key = min(key0 + in / CK, nk - 1), c = in % CK;
-            if (KALL >= kThreads || tid < KALL)
-                kr[i] = *reinterpret_cast<const v4u *>(a.k + ((size_t)(k0 + key) * 2 * H + kb * H + h) * D + c * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < VP; ++i) {
-            const int at = i * kThreads + tid, key = key0 + at / (D / 4) * 4, c = at % (D / 4);
-            if (VALL >= kThreads || tid < VALL) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    vr[i][j] = *reinterpret_cast<const uint2 *>(a.v + ((size_t)(k0 + min(key + j, nk - 1)) * H + h) * D + c * 4);
+            for (int i = 0; i < KP; ++i) {
+                // (piece i * kThreads + tid: so many rows, or the other K, further on)
+                constexpr int HALF = KALL / 2;
+                const unsigned more = (unsigned)(i * kThreads % HALF / CK) * k_row + (unsigned)(i * kThreads / HALF * H * D) * 2;
+                kr[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(r, (int)k_off, (int)more, 0));
             }
         }
-        if (a.doc_k && tid < S::kKeys) doc_r = key0 + tid < nk ? a.doc_k[k0 + key0 + tid] : -1;
     };
-    // Into LDS; V as columns of keys, the keys of a step of 16 in the order 0-3, 8-11, 4-7, 12-15.
-    auto deposit = [&](int buf) {
-        _Float16 *kb = lds + buf * S::kHalves, *vb = kb + 2 * S::kK;
+    auto request_v = [&](int tile) {
+        const rsrc_t r = rows_of(a.v, v_row, tile * S::kKeys);
+        if (VALL >= kThreads || tid < VALL) {
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            const int at = i * kThreads + tid;
-            if (KALL >= kThreads || tid < KALL)
-                reinterpret_cast<v4u *>(kb + at / (KALL / 2) * S::kK)[k_chunk<CK>(at % (KALL / 2) / CK, at % CK)] = kr[i];
+            for (int i = 0; i < VP; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    vr[i][j] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(
+                                                             r, (int)v_off, (int)((unsigned)(i * (kThreads / (D / 4)) * 4 + j) * v_row), 0));
         }
-        bool odd = false;
+        if (a.doc_k && tid < S::kKeys) {
+            const int key = tile * S::kKeys + tid;
+            doc_r = key < nk ? a.doc_k[k0 + key] : -1;
+        }
+    };
+    auto deposit_k = [&](int buf) {
+        _Float16 *kb = lds + buf * 2 * S::kK;
+        if (KALL >= kThreads || tid < KALL) {
 #pragma unroll
-        for (int i = 0; i < VP; ++i) {
-            const int at = i * kThreads + tid, quad = at / (D / 4), c = at % (D / 4);
-            if (VALL >= kThreads || tid < VALL) {
+            for (int i = 0; i < KP; ++i) {
+                const int at = i * kThreads + tid;
+                reinterpret_cast<v4u *>(kb + at / (KALL / 2) * S::kK)[k_chunk<CK>(at % (KALL / 2) / CK, at % CK)] = kr[i];
+            }
+        }
+    };
+    // V as columns of keys, the keys of a step of 16 in the order 0-3, 8-11, 4-7, 12-15.
+    auto deposit_v = [&](int buf) {
+        _Float16 *vb = lds + S::kBufs * 2 * S::kK + buf * S::kV;
+        bool odd = false;
+        if (VALL >= kThreads || tid < VALL) {
+#pragma unroll
+            for (int i = 0; i < VP; ++i) {
+                const int at = i * kThreads + tid, quad = at / (D / 4), c = at % (D / 4);
                 const int place = (quad & ~3) + ((quad & 1) << 1 | (quad & 2) >> 1);    // 8-byte place in a column
-                uint32_t o = 0;
+                v2h o = {(_Float16)0.0f, (_Float16)0.0f};           // 0 * x: what is no finite number leaves a NaN
+                const v2h zero = o;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    asm("v_pk_max_u16 %0, %1, %2" : "=v"(o) : "v"(o), "v"(vr[i][j].x & 0x7fff7fffu));
-                    asm("v_pk_max_u16 %0, %1, %2" : "=v"(o) : "v"(o), "v"(vr[i][j].y & 0x7fff7fffu));
+                    o = __builtin_elementwise_fma(__builtin_bit_cast(v2h, vr[i][j].x), zero, o);
+                    o = __builtin_elementwise_fma(__builtin_bit_cast(v2h, vr[i][j].y), zero, o);
                 }
-                if (odd_magnitudes(o)) {
+                if ((__builtin_bit_cast(uint32_t, o) & 0x7fff7fffu) != 0) {
                     odd = true;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -229,30 +258,61 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         if (l == 0) odd_s[buf][w] = any ? 1 : 0;
     };
 
+    auto request = [&](int tile) {
+        request_k(tile);
+        request_v(tile);
+    };
+    auto deposit = [&](int buf) {
+        deposit_k(buf);
+        deposit_v(buf);
+    };
+
     float m = -INFINITY, sum = 0.0f;
     v16f o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+    const int sub0 = split * SUB;                   // the wavefront's groups of 32 keys in a tile
+    // its operands' places in LDS: of K for chunk 2 st + half (another chunk of 8 is 128 bytes further on, 32 rows are
+    // a constant too), of V for the even and the odd row tiles of O^T
+    constexpr int KA = KS < 4 ? KS : 4;
+    int k_at[KA], v_at[2][SUB * 2];
+#pragma unroll
+    for (int st = 0; st < KA; ++st) k_at[st] = br * S::kK + k_chunk<CK>(sub0 * 32 + col, st * 2 + half) * 8;
+#pragma unroll
+    for (int par = 0; par < 2; ++par)
+#pragma unroll
+        for (int st = 0; st < SUB * 2; ++st)
+            v_at[par][st] = SPLIT == 1 && par ? v_at[0][st ^ 2] : (v_chunk<CV>(par * 32 + col, (sub0 * 2 + st) * 2 + half) - par * 32 * CV) * 8;
 
-    // `same`: every key of the tile has the one document of all the rows
-    auto compute = [&](int tile, int buf, bool same) {
-        const int sub0 = split * SUB, key0 = tile * S::kKeys + sub0 * 32;           // the wavefront's keys of the tile
-        if (key0 >= most) return;
-        const _Float16 *kb = lds + buf * S::kHalves + br * S::kK, *vb = lds + buf * S::kHalves + 2 * S::kK;
-        const bool docs = a.doc_k && !same;
-        v16f s[SUB];
+    auto scores = [&](int buf, v16f (&x)[SUB]) {
+        const _Float16 *kb = lds + buf * 2 * S::kK;
+        constexpr int KB = D == 128 ? 1 : SUB;          // groups of 32 keys whose operands are requested together
 #pragma unroll
-        for (int kt = 0; kt < SUB; ++kt) {
+        for (int k1 = 0; k1 < SUB; k1 += KB) {
+            v8h f[KB][KS];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[kt][e] = 0.0f;
+            for (int kt = 0; kt < KB; ++kt)
 #pragma unroll
-            for (int st = 0; st < KS; ++st) {
-                const v8h x = *reinterpret_cast<const v8h *>(kb + k_chunk<CK>((sub0 + kt) * 32 + col, st * 2 + half) * 8);
-                s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[st], s[kt], 0, 0, 0);
+                for (int st = 0; st < KS; ++st)
+                    f[kt][st] = *reinterpret_cast<const v8h *>(kb + k_at[st % KA] + ((k1 + kt) * 32 * CK + st / KA * 8) * 8);
+#pragma unroll
+            for (int kt = 0; kt < KB; ++kt) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[k1 + kt][e] = 0.0f;
+#pragma unroll
+                for (int st = 0; st < KS; ++st) x[k1 + kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[kt][st], q[st], x[k1 + kt], 0, 0, 0);
             }
         }
+    };
+    // One tile.  MASKED: some row may not see some key.
+    auto compute = [&](auto masked, int tile, int buf, bool same) {
+        constexpr bool MASKED = decltype(masked)::value;
+        const int key0 = tile * S::kKeys + sub0 * 32;
+        const _Float16 *vb = lds + S::kBufs * 2 * S::kK + buf * S::kV;
+        v16f s[SUB];
+        scores(buf, s);
         // in base 2 from here on: s * unit
         if (MOD) {
             if (cap > 0.0f) {
@@ -287,24 +347,25 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                         s[kt][e] = __builtin_fmaf(-slope, fabsf(away - (float)(kt * 32 + 8 * (e >> 2) + (e & 3))), s[kt][e]);
             }
         }
-        if (docs) {
+        if (MASKED) {
             const int left = opaque(limit - key0 - 4 * half);
-            const v4i *ids = reinterpret_cast<const v4i *>(doc_s[buf] + sub0 * 32 + opaque(4 * half));
+            if (a.doc_k && !same) {
+                const v4i *ids = reinterpret_cast<const v4i *>(doc_s[buf] + sub0 * 32 + opaque(4 * half));
 #pragma unroll
-            for (int kt = 0; kt < SUB; ++kt)
+                for (int kt = 0; kt < SUB; ++kt)
 #pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    const v4i id = ids[kt * 8 + e4 * 2];
+                    for (int e4 = 0; e4 < 4; ++e4) {
+                        const v4i id = ids[kt * 8 + e4 * 2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[kt][e4 * 4 + e] = kt * 32 + 8 * e4 + e < left && id[e] == doc ? s[kt][e4 * 4 + e] : -INFINITY;
-                }
-        } else if (key0 + SUB * 32 > least) {
-            const int left = opaque(limit - key0 - 4 * half);
+                        for (int e = 0; e < 4; ++e)
+                            s[kt][e4 * 4 + e] = kt * 32 + 8 * e4 + e < left && id[e] == doc ? s[kt][e4 * 4 + e] : -INFINITY;
+                    }
+            } else {
 #pragma unroll
-            for (int kt = 0; kt < SUB; ++kt)
+                for (int kt = 0; kt < SUB; ++kt)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[kt][e] = kt * 32 + 8 * (e >> 2) + (e & 3) < left ? s[kt][e] : -INFINITY;
+                    for (int e = 0; e < 16; ++e) s[kt][e] = kt * 32 + 8 * (e >> 2) + (e & 3) < left ? s[kt][e] : -INFINITY;
+            }
         }
         float top = s[0][0];
 #pragma unroll
@@ -324,11 +385,20 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 for (int e = 0; e < 16; ++e) o[t][e] *= corr;
         }
         const float base = kLift - (m == -INFINITY ? 0.0f : m);
-        v8h pr[SUB * 2];                                // the weights, operand B of O^T
+        constexpr int VB = DT > 2 ? 2 : DT;             // row tiles of O^T whose operands are requested together
+        v8h vx[VB][SUB * 2], pr[SUB * 2];
+        auto load_v = [&](int t1) {
+#pragma unroll
+            for (int t = 0; t < VB; ++t)
+#pragma unroll
+                for (int st = 0; st < SUB * 2; ++st)
+                    vx[t][st] = *reinterpret_cast<const v8h *>(vb + v_at[(t1 + t) & 1][st] + (t1 + t) * 32 * CV * 8);
+        };
+        load_v(0);
 #pragma unroll
         for (int kt = 0; kt < SUB; ++kt)
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
+            for (int e = 0; e < 16; e += 2) {           // the weights, operand B of O^T
                 v2f x;
                 x[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e], unit, base));
                 x[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e + 1], unit, base));
@@ -338,12 +408,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 pr[kt * 2 + (e >> 3)][(e & 7) + 1] = y[1];
             }
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+        for (int t1 = 0; t1 < DT; t1 += VB) {
+            if (t1 > 0) load_v(t1);
 #pragma unroll
-            for (int st = 0; st < SUB * 2; ++st) {
-                const v8h x = *reinterpret_cast<const v8h *>(vb + v_chunk<CV>(t * 32 + col, (sub0 * 2 + st) * 2 + half) * 8);
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pr[st], o[t], 0, 0, 0);
-            }
+            for (int st = 0; st < SUB * 2; ++st)
+#pragma unroll
+                for (int t = 0; t < VB; ++t) o[t1 + t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vx[t][st], pr[st], o[t1 + t], 0, 0, 0);
+        }
         int odd = 0;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) odd |= odd_s[buf][i];
@@ -370,8 +441,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 
     // ---- the keys, in windows: all of them, or 64 tiles at a time of which those are taken whose documents can matter
     for (int from = 0; from < tiles; from += 64) {
-        unsigned long long visit = 0, same = 0;
-        int tile = 0;
+        unsigned long long visit = 0, uniform = 0;
         if (a.doc_k) {
             constexpr int EACH = S::kKeys / kWaves;     // a lane looks at so many keys of tile from + l
             int lo = INT_MAX, hi = INT_MIN;
@@ -390,31 +460,37 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 hi = max(hi, win_hi[i][l]);
             }
             visit = __ballot(from + l < tiles && hi >= doc_lo && lo <= doc_hi);
-            same = __ballot(lo == hi && lo == doc_lo && lo == doc_hi);
-            if (visit) tile = from + __builtin_ctzll(visit);
+            uniform = __ballot(lo == hi && lo == doc_lo && lo == doc_hi);
             __syncthreads();                            // (the window's arrays are read before the next window's are written)
             if (!visit) continue;
         }
+        const int stop = a.doc_k ? min(from + 64, tiles) : tiles;
+        int tile = a.doc_k ? from + (int)__builtin_ctzll(visit) : 0, buf = 0;
         request(tile);
         deposit(0);
         __syncthreads();
-        int buf = 0;
-        while (tile < tiles) {
+        auto step = [&](auto masked) {
             int next = tile + 1;
-            bool one = false;
+            bool same = false;
             if (a.doc_k) {
-                one = (same >> (tile - from)) & 1;
+                same = (uniform >> (tile - from)) & 1;
                 visit &= visit - 1;
-                next = visit ? from + __builtin_ctzll(visit) : tiles;
+                next = visit ? from + (int)__builtin_ctzll(visit) : stop;
             }
-            if (next < tiles) request(next);
-            compute(tile, buf, one);
+            if (next < stop) request(next);
+            if (!decltype(masked)::value || tile * S::kKeys + sub0 * 32 < most) compute(masked, tile, buf, same);
             if (S::kBufs == 1) __syncthreads();
-            if (S::kBufs == 2) buf ^= 1;
-            if (next < tiles) deposit(buf);
+            else buf ^= 1;
+            if (next < stop) deposit(buf);
             __syncthreads();
             tile = next;
+        };
+        // (a loop for the tiles that every row sees whole, and one for the others: what differs between them inside one loop costs
+        // copies of the accumulators)
+        if (!a.doc_k) {
+            while (tile < whole) step(std::false_type{});
         }
+        while (tile < stop) step(std::true_type{});
         if (!a.doc_k) break;
     }
 
