@@ -31,6 +31,7 @@ namespace {
 
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kThreads = 512, kWaves = kThreads / 64;
@@ -47,26 +48,23 @@ struct PrefillParams {
 // Sizes of one variant.
 template <int D, int SPLIT>
 struct Shape {
-    static constexpr int kRows = 128 / SPLIT, kKeys = SPLIT == 1 ? 64 : 128;
+    static constexpr int kRows = 128 / SPLIT, kGroups = 4 / SPLIT;         // rows, and groups of 32 of them
+    static constexpr int kKeys = SPLIT == 1 ? 64 : 32 * SPLIT;
     static constexpr int kSub = kKeys / 32 / SPLIT;             // groups of 32 keys per wavefront and tile
-    static constexpr int kChunksK = D / 8, kChunksV = kKeys / 8;
-    static constexpr int kK = kKeys * D, kV = (D < 32 ? 32 : D) * kKeys, kHalves = 2 * kK + kV;
-    static constexpr int kBufs = 2 * kHalves * 2 <= 147456 ? 2 : 1;
+    static constexpr int kChunks = D / 8;                       // 16-byte chunks of a row of K or V
+    static constexpr int kK = kKeys * D, kHalves = 3 * kK;      // a tile: K1, K2, V
     static constexpr int kTileT = (D + 31) / 32;                // row tiles of O^T
     // outputs on their way between wavefronts, in the tiles' place
-    static constexpr size_t kLds = (size_t)kBufs * kHalves * 2;
-    static_assert((size_t)(SPLIT == 1 ? 4 : 6) * kTileT * 4096 <= kLds, "the merge fits where the tiles were");
+    static constexpr size_t kMerge = (size_t)(SPLIT == 1 ? 4 : 2 * (SPLIT - 1) * kGroups) * kTileT * 4096;
+    static constexpr size_t kLds = (size_t)2 * kHalves * 2 > kMerge ? (size_t)2 * kHalves * 2 : kMerge;
 };
 
-// Place of a 16-byte chunk of row `row` of K, and of column d of V, so that the eight rows that are read together lie in
-// different banks.
+// Where a 16-byte chunk of a row of K and of V lies in the row, so that the rows that are read together lie in different
+// banks (its own inverse).
 template <int C>
-__device__ inline int k_chunk(int row, int c)
-{
-    return row * C + (C >= 8 ? c ^ (row & 7) : C == 4 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1));
-}
+__device__ inline int k_swap(int row, int c) { return C >= 8 ? c ^ (row & 7) : C == 4 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1); }
 template <int C>
-__device__ inline int v_chunk(int d, int c) { return d * C + (c ^ ((d ^ (d >> 3)) & 7)); }
+__device__ inline int v_swap(int row, int c) { return C >= 8 ? c ^ ((row & 1) << 2) : c; }
 
 // A value that the compiler does not see through: what rare paths compute from it is computed there, instead of being kept
 // in registers across the loop.
@@ -86,19 +84,18 @@ template <int D, bool MOD, int SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams p)
 {
     using S = Shape<D, SPLIT>;
-    constexpr int KS = D / 16, DT = S::kTileT, SUB = S::kSub, CK = S::kChunksK, CV = S::kChunksV;
-    constexpr int KP = 2 * S::kKeys * CK / kThreads > 0 ? 2 * S::kKeys * CK / kThreads : 1;     // 16-byte pieces of K per thread
-    constexpr int KALL = 2 * S::kKeys * CK;
-    constexpr int VALL = S::kKeys * D / 16, VP = VALL > kThreads ? VALL / kThreads : 1;         // 4 x 4 pieces of V per thread
+    constexpr int KS = D / 16, DT = S::kTileT, SUB = S::kSub, C = S::kChunks;
+    constexpr int KI = 2 * S::kKeys * C / 64, VI = S::kKeys * C / 64;           // KiB of K1 and K2, and of V, in a tile
+    constexpr int KP = KI > kWaves ? KI / kWaves : 1, VP = VI > kWaves ? VI / kWaves : 1;       // of them per wavefront
     extern __shared__ __align__(16) _Float16 lds[];
-    __shared__ int odd_s[2][kWaves], doc_s[2][S::kKeys];
+    __shared__ int odd_s[2], doc_s[2][S::kKeys];
     __shared__ int most_s[kWaves], least_s[kWaves], lo_s[kWaves], hi_s[kWaves], win_lo[kWaves][64], win_hi[kWaves][64];
-    __shared__ float m_s[SPLIT][2][32], sum_s[SPLIT][2][32];
+    __shared__ float m_s[SPLIT][2][S::kGroups][32], sum_s[SPLIT][2][S::kGroups][32];
     const PrefillArgs &a = p.a;
     const int H = a.n_heads, h = blockIdx.x % H;
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = l >> 5, col = l & 31;
-    const int br = w >> 2, group = SPLIT == 1 ? w & 3 : 0, split = SPLIT == 1 ? 0 : w & 3;
+    const int br = w >> 2, group = (w & 3) % S::kGroups, split = (w & 3) / S::kGroups;
 
     // ---- which rows: the slots of sequence b begin at cu_q[b] / kRows + b; the last ones first (they see the most keys)
     const int slot = p.slots - 1 - (int)(blockIdx.x / H);
@@ -132,6 +129,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 hi = max(hi, __shfl_xor(hi, o, 64));
             }
         }
+        if (tid < 2) odd_s[tid] = -1;
         if (l == 0) {
             most_s[w] = most;
             least_s[w] = least;
@@ -166,105 +164,66 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     const float unit = MOD ? 1.0f : p.scale * kLog2e;
     const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};
 
-    // ---- tiles on their way: global memory -> registers -> LDS.
-    // A tile's rows are read through a descriptor that ends where the sequence does: rows behind it are zeros, and what a
-    // thread adds to the tile's address does not change from tile to tile.
+    // ---- tiles on their way: K straight from memory into LDS, V through registers, where it is looked through for values that
+    // are no finite numbers.  A tile's rows are read through a descriptor that ends where the sequence does: rows
+    // behind it are zeros, and what a lane adds to the tile's address does not change from tile to tile.
     const unsigned k_row = (unsigned)H * D * 4, v_row = (unsigned)H * D * 2;
     auto rows_of = [&](const _Float16 *base, unsigned row_bytes, int key0) {
         return make_rsrc(reinterpret_cast<const char *>(base) + (size_t)(k0 + key0) * row_bytes, (unsigned)min(nk - key0, S::kKeys) * row_bytes);
     };
-    v4u kr[KP];
-    uint2 vr[VP][4];
+    // KiB i * kWaves + w of a tile, 64 chunks, is the wavefront's; further ones are a constant number of rows (or the other K) on
+    const int chunk = w * 64 + l, v_lds = chunk / C * D + v_swap<C>(chunk / C, chunk % C) * 8;
+    const int k_in = chunk % (S::kKeys * C);
+    const unsigned k_off = (unsigned)(k_in / C) * k_row + (unsigned)((chunk / (S::kKeys * C) * H + h) * D + k_swap<C>(k_in / C, k_in % C) * 8) * 2;
+    const unsigned v_off = (unsigned)(chunk / C) * v_row + (unsigned)(h * D + chunk % C * 8) * 2;
+    v4u vr[VP];
     int doc_r = 0;
-    const unsigned k_off = (unsigned)(tid % (KALL / 2) / CK) * k_row + (unsigned)((tid / (KALL / 2) * H + h) * D + tid % CK * 8) * 2;
-    const unsigned v_off = (unsigned)(tid / (D / 4) * 4) * v_row + (unsigned)(h * D + tid % (D / 4) * 4) * 2;
-    auto request_k = [&](int tile) {
+    auto request = [&](int tile, int buf) {
         const rsrc_t r = rows_of(a.k, k_row, tile * S::kKeys);
-        if (KALL >= kThreads || tid < KALL) {
+        _Float16 *kb = lds + buf * S::kHalves;
+        if (KI >= kWaves || w < KI) {
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
-                // (piece i * kThreads + tid: so many rows, or the other K, further on)
-                constexpr int HALF = KALL / 2;
-                const unsigned more = (unsigned)(i * kThreads % HALF / CK) * k_row + (unsigned)(i * kThreads / HALF * H * D) * 2;
-                kr[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(r, (int)k_off, (int)more, 0));
+                constexpr int HALF = KI / 2;
+                const unsigned more = (unsigned)(i * kWaves % HALF * 64 / C) * k_row + (unsigned)(i * kWaves / HALF * H * D) * 2;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(kb + (i * kWaves + w) * 512), 16, (int)k_off, (int)more, 0, 0);
             }
         }
-    };
-    auto request_v = [&](int tile) {
-        const rsrc_t r = rows_of(a.v, v_row, tile * S::kKeys);
-        if (VALL >= kThreads || tid < VALL) {
+        const rsrc_t rv = rows_of(a.v, v_row, tile * S::kKeys);
+        if (VI >= kWaves || w < VI) {
 #pragma unroll
             for (int i = 0; i < VP; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    vr[i][j] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(
-                                                             r, (int)v_off, (int)((unsigned)(i * (kThreads / (D / 4)) * 4 + j) * v_row), 0));
+                vr[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rv, (int)v_off, (int)((unsigned)(i * kWaves * 64 / C) * v_row), 0));
         }
         if (a.doc_k && tid < S::kKeys) {
             const int key = tile * S::kKeys + tid;
             doc_r = key < nk ? a.doc_k[k0 + key] : -1;
         }
     };
-    auto deposit_k = [&](int buf) {
-        _Float16 *kb = lds + buf * 2 * S::kK;
-        if (KALL >= kThreads || tid < KALL) {
-#pragma unroll
-            for (int i = 0; i < KP; ++i) {
-                const int at = i * kThreads + tid;
-                reinterpret_cast<v4u *>(kb + at / (KALL / 2) * S::kK)[k_chunk<CK>(at % (KALL / 2) / CK, at % CK)] = kr[i];
-            }
-        }
-    };
-    // V as columns of keys, the keys of a step of 16 in the order 0-3, 8-11, 4-7, 12-15.
-    auto deposit_v = [&](int buf) {
-        _Float16 *vb = lds + S::kBufs * 2 * S::kK + buf * S::kV;
-        bool odd = false;
-        if (VALL >= kThreads || tid < VALL) {
+    auto deposit = [&](int tile, int buf) {
+        _Float16 *vb = lds + buf * S::kHalves + 2 * S::kK;
+        if (VI >= kWaves || w < VI) {
 #pragma unroll
             for (int i = 0; i < VP; ++i) {
-                const int at = i * kThreads + tid, quad = at / (D / 4), c = at % (D / 4);
-                const int place = (quad & ~3) + ((quad & 1) << 1 | (quad & 2) >> 1);    // 8-byte place in a column
-                v2h o = {(_Float16)0.0f, (_Float16)0.0f};           // 0 * x: what is no finite number leaves a NaN
-                const v2h zero = o;
+                v2h x = {(_Float16)0.0f, (_Float16)0.0f};           // 0 * v: what is no finite number leaves a NaN
+                const v2h zero = x;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    o = __builtin_elementwise_fma(__builtin_bit_cast(v2h, vr[i][j].x), zero, o);
-                    o = __builtin_elementwise_fma(__builtin_bit_cast(v2h, vr[i][j].y), zero, o);
-                }
-                if ((__builtin_bit_cast(uint32_t, o) & 0x7fff7fffu) != 0) {
-                    odd = true;
+                for (int j = 0; j < 4; ++j) x = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (uint32_t)vr[i][j]), zero, x);
+                if ((__builtin_bit_cast(uint32_t, x) & 0x7fff7fffu) != 0) {
+                    odd_s[buf] = tile;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        auto clean = [](uint32_t x) {
-                            if ((x & 0x7c00u) == 0x7c00u) x &= 0xffff0000u;
-                            if ((x & 0x7c000000u) == 0x7c000000u) x &= 0x0000ffffu;
-                            return x;
-                        };
-                        vr[i][j].x = clean(vr[i][j].x);
-                        vr[i][j].y = clean(vr[i][j].y);
+                        uint32_t y = vr[i][j];
+                        if ((y & 0x7c00u) == 0x7c00u) y &= 0xffff0000u;
+                        if ((y & 0x7c000000u) == 0x7c000000u) y &= 0x0000ffffu;
+                        vr[i][j] = y;
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-                    auto word = [&](int j) { return e < 2 ? vr[i][j].x : vr[i][j].y; };
-                    const uint2 x = make_uint2(__builtin_amdgcn_perm(word(1), word(0), sel), __builtin_amdgcn_perm(word(3), word(2), sel));
-                    *reinterpret_cast<uint2 *>(vb + v_chunk<CV>(c * 4 + e, place >> 1) * 8 + (place & 1) * 4) = x;
-                }
+                *reinterpret_cast<v4u *>(vb + v_lds + i * kWaves * 64 / C * D) = vr[i];
             }
         }
         if (a.doc_k && tid < S::kKeys) doc_s[buf][tid] = doc_r;
-        const bool any = __any(odd);
-        if (l == 0) odd_s[buf][w] = any ? 1 : 0;
-    };
-
-    auto request = [&](int tile) {
-        request_k(tile);
-        request_v(tile);
-    };
-    auto deposit = [&](int buf) {
-        deposit_k(buf);
-        deposit_v(buf);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // K lies in LDS
     };
 
     float m = -INFINITY, sum = 0.0f;
@@ -274,20 +233,23 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
     const int sub0 = split * SUB;                   // the wavefront's groups of 32 keys in a tile
-    // its operands' places in LDS: of K for chunk 2 st + half (another chunk of 8 is 128 bytes further on, 32 rows are
-    // a constant too), of V for the even and the odd row tiles of O^T
+    // its operands' places in LDS: of K for chunk 2 st + half (another eight chunks are 128 bytes further on, 32 rows
+    // are a constant too); of V for the even and odd row tiles of O^T, where lane j of 16 asks for 4 columns of key j / 4, and gets
+    // 4 keys of column j
     constexpr int KA = KS < 4 ? KS : 4;
-    int k_at[KA], v_at[2][SUB * 2];
+    int k_at[KA], v_at[2];
 #pragma unroll
-    for (int st = 0; st < KA; ++st) k_at[st] = br * S::kK + k_chunk<CK>(sub0 * 32 + col, st * 2 + half) * 8;
+    for (int st = 0; st < KA; ++st) k_at[st] = br * S::kK + (sub0 * 32 + col) * D + k_swap<C>(col, st * 2 + half) * 8;
+    {
+        const int key = 4 * half + (l >> 2 & 3), c4 = D < 32 ? l & 3 : (l >> 4 & 1) * 4 + (l & 3);  // quad of columns
 #pragma unroll
-    for (int par = 0; par < 2; ++par)
-#pragma unroll
-        for (int st = 0; st < SUB * 2; ++st)
-            v_at[par][st] = SPLIT == 1 && par ? v_at[0][st ^ 2] : (v_chunk<CV>(par * 32 + col, (sub0 * 2 + st) * 2 + half) - par * 32 * CV) * 8;
+        for (int par = 0; par < 2; ++par) v_at[par] = (sub0 * 32 + key) * D + v_swap<C>(key, (D < 64 ? 0 : par * 4) + c4 / 2) * 8 + (c4 & 1) * 4;
+    }
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s *lds_v4s_t;
 
     auto scores = [&](int buf, v16f (&x)[SUB]) {
-        const _Float16 *kb = lds + buf * 2 * S::kK;
+        const _Float16 *kb = lds + buf * S::kHalves;
         constexpr int KB = D == 128 ? 1 : SUB;          // groups of 32 keys whose operands are requested together
 #pragma unroll
         for (int k1 = 0; k1 < SUB; k1 += KB) {
@@ -296,7 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             for (int kt = 0; kt < KB; ++kt)
 #pragma unroll
                 for (int st = 0; st < KS; ++st)
-                    f[kt][st] = *reinterpret_cast<const v8h *>(kb + k_at[st % KA] + ((k1 + kt) * 32 * CK + st / KA * 8) * 8);
+                    f[kt][st] = *reinterpret_cast<const v8h *>(kb + k_at[st % KA] + (k1 + kt) * 32 * D + st / KA * 64);
 #pragma unroll
             for (int kt = 0; kt < KB; ++kt) {
 #pragma unroll
@@ -310,7 +272,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     auto compute = [&](auto masked, int tile, int buf, bool same) {
         constexpr bool MASKED = decltype(masked)::value;
         const int key0 = tile * S::kKeys + sub0 * 32;
-        const _Float16 *vb = lds + S::kBufs * 2 * S::kK + buf * S::kV;
+        _Float16 *vb = lds + buf * S::kHalves + 2 * S::kK;
         v16f s[SUB];
         scores(buf, s);
         // in base 2 from here on: s * unit
@@ -391,8 +353,12 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 #pragma unroll
             for (int t = 0; t < VB; ++t)
 #pragma unroll
-                for (int st = 0; st < SUB * 2; ++st)
-                    vx[t][st] = *reinterpret_cast<const v8h *>(vb + v_at[(t1 + t) & 1][st] + (t1 + t) * 32 * CV * 8);
+                for (int st = 0; st < SUB * 2; ++st) {
+                    _Float16 *at = vb + v_at[(t1 + t) & 1] + (t1 + t) / 2 * 64 + st * 16 * D;
+                    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)at);
+                    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(at + 8 * D));
+                    vx[t][st] = __builtin_bit_cast(v8h, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
         };
         load_v(0);
 #pragma unroll
@@ -415,10 +381,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 #pragma unroll
                 for (int t = 0; t < VB; ++t) o[t1 + t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vx[t][st], pr[st], o[t1 + t], 0, 0, 0);
         }
-        int odd = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) odd |= odd_s[buf][i];
-        if (__builtin_amdgcn_readfirstlane(odd)) {
+        if (__builtin_amdgcn_readfirstlane(odd_s[buf]) == tile) {
             // values that are no finite numbers, to the rows that see them
             const int n = min(SUB * 32, nk - key0);
             for (int j = 0; j < n; ++j) {
@@ -466,8 +429,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         }
         const int stop = a.doc_k ? min(from + 64, tiles) : tiles;
         int tile = a.doc_k ? from + (int)__builtin_ctzll(visit) : 0, buf = 0;
-        request(tile);
-        deposit(0);
+        request(tile, 0);
+        deposit(tile, 0);
         __syncthreads();
         auto step = [&](auto masked) {
             int next = tile + 1;
@@ -477,11 +440,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 visit &= visit - 1;
                 next = visit ? from + (int)__builtin_ctzll(visit) : stop;
             }
-            if (next < stop) request(next);
+            if (next < stop) request(next, buf ^ 1);
             if (!decltype(masked)::value || tile * S::kKeys + sub0 * 32 < most) compute(masked, tile, buf, same);
-            if (S::kBufs == 1) __syncthreads();
-            else buf ^= 1;
-            if (next < stop) deposit(buf);
+            buf ^= 1;
+            if (next < stop) deposit(next, buf);
             __syncthreads();
             tile = next;
         };
@@ -500,24 +462,24 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     auto place = [&](int i, int t, int e) { return ((i * DT + t) * 16 + e) * 64 + l; };
     if (SPLIT > 1) {
         if (l < 32) {
-            m_s[split][br][col] = m;
-            sum_s[split][br][col] = sum;
+            m_s[split][br][group][col] = m;
+            sum_s[split][br][group][col] = sum;
         }
         __syncthreads();
         float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < SPLIT; ++i) top = fmaxf(top, m_s[i][br][col]);
+        for (int i = 0; i < SPLIT; ++i) top = fmaxf(top, m_s[i][br][group][col]);
         top = top == -INFINITY ? 0.0f : top;
         sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < SPLIT; ++i) sum += sum_s[i][br][col] * __builtin_amdgcn_exp2f(m_s[i][br][col] - top);
+        for (int i = 0; i < SPLIT; ++i) sum += sum_s[i][br][group][col] * __builtin_amdgcn_exp2f(m_s[i][br][group][col] - top);
         const float f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 o[t][e] *= f;
-                if (split > 0) xchg[place((split - 1) * 2 + br, t, e)] = o[t][e];
+                if (split > 0) xchg[place(((split - 1) * 2 + br) * S::kGroups + group, t, e)] = o[t][e];
             }
         __syncthreads();
         if (split == 0) {
@@ -526,7 +488,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 #pragma unroll
                 for (int t = 0; t < DT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[t][e] += xchg[place(i * 2 + br, t, e)];
+                    for (int e = 0; e < 16; ++e) o[t][e] += xchg[place((i * 2 + br) * S::kGroups + group, t, e)];
         }
         __syncthreads();
     }
@@ -560,7 +522,8 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
     p.a = a;
     p.scale = 1.0f / sqrtf((float)d_h);
     const bool mod = a.softcap > 0.0f || a.slopes;
-    // fewer workgroups of 128 rows than the chip holds at a time: 32 rows each
+    // fewer workgroups of 128 rows than the chip holds at a time: 32 rows each (128 columns, for whose tiles of 128 keys LDS has no
+    // room twice: 64 rows)
     const bool few = (long long)(a.Tq / 128 + a.B) * a.n_heads < 512;
     hipError_t e = hipSuccess;
     auto go = [&](auto d, auto m, auto split) {
@@ -574,7 +537,7 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
             hipLaunchKernelGGL((prefill_attn_kernel<D, MOD, SPLIT>), dim3((unsigned)p.slots * a.n_heads), dim3(kThreads), S::kLds, st, p);
     };
     auto variant = [&](auto d, auto m) {
-        if (few) go(d, m, std::integral_constant<int, 4>{});
+        if (few) go(d, m, std::integral_constant<int, decltype(d)::value == 128 ? 2 : 4>{});
         else go(d, m, std::integral_constant<int, 1>{});
     };
     auto both = [&](auto d) {
