@@ -56,7 +56,8 @@ struct Shape {
     static constexpr int kTileT = (D + 31) / 32;                // row tiles of O^T
     // outputs on their way between wavefronts, in the tiles' place
     static constexpr size_t kMerge = (size_t)(SPLIT == 1 ? 4 : 2 * (SPLIT - 1) * kGroups) * kTileT * 4096;
-    static constexpr size_t kLds = (size_t)2 * kHalves * 2 > kMerge ? (size_t)2 * kHalves * 2 : kMerge;
+    static constexpr size_t kTiles = (size_t)3 * kHalves * 2;
+    static constexpr size_t kLds = kTiles > kMerge ? kTiles : kMerge;
 };
 
 // Where a 16-byte chunk of a row of K and of V lies in the row, so that the rows that are read together lie in different
@@ -64,7 +65,7 @@ struct Shape {
 template <int C>
 __device__ inline int k_swap(int row, int c) { return C >= 8 ? c ^ (row & 7) : C == 4 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1); }
 template <int C>
-__device__ inline int v_swap(int row, int c) { return C >= 8 ? c ^ ((row & 1) << 2) : c; }
+__device__ inline int v_swap(int row, int c) { return C >= 8 ? c ^ ((row & 3) << 1) : C == 4 ? c ^ (row & 2) : c; }
 
 // A value that the compiler does not see through: what rare paths compute from it is computed there, instead of being kept
 // in registers across the loop.
@@ -74,6 +75,20 @@ __device__ inline int opaque(int v)
     return v;
 }
 // The larger of a lane's value and of the lane 32 further on or back.
+// 64 x 16 bytes from memory straight into LDS, in flight until a wait on vmcnt.  (In assembly because with the builtin the compiler
+// waits for everything in flight before the transposing LDS reads, whichever buffer they read.  Nothing comes back in
+// registers, and the kernel's own waits are the only ones that are needed.)
+__device__ inline void load_to_lds(v4u rsrc, unsigned lds_byte, unsigned lane_off, unsigned off)
+{
+    unsigned kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds_byte), "v"(lane_off), "s"(rsrc), "s"(off) : "memory");
+}
+__device__ inline v4u rsrc_words(const void *base, unsigned bytes)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(base);
+    return v4u{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, bytes, 0x00020000u};
+}
 __device__ inline float halves_max(float v)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
@@ -88,7 +103,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     constexpr int KI = 2 * S::kKeys * C / 64, VI = S::kKeys * C / 64;           // KiB of K1 and K2, and of V, in a tile
     constexpr int KP = KI > kWaves ? KI / kWaves : 1, VP = VI > kWaves ? VI / kWaves : 1;       // of them per wavefront
     extern __shared__ __align__(16) _Float16 lds[];
-    __shared__ int odd_s[2], doc_s[2][S::kKeys];
+    __shared__ int odd_s[3], doc_s[3][S::kKeys];
     __shared__ int most_s[kWaves], least_s[kWaves], lo_s[kWaves], hi_s[kWaves], win_lo[kWaves][64], win_hi[kWaves][64];
     __shared__ float m_s[SPLIT][2][S::kGroups][32], sum_s[SPLIT][2][S::kGroups][32];
     const PrefillArgs &a = p.a;
@@ -129,7 +144,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 hi = max(hi, __shfl_xor(hi, o, 64));
             }
         }
-        if (tid < 2) odd_s[tid] = -1;
+        if (tid < 3) odd_s[tid] = -1;
         if (l == 0) {
             most_s[w] = most;
             least_s[w] = least;
@@ -158,72 +173,78 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h *>(src + s * 16);
     }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));     // (they are waited for here, not in the loop)
     const float cap = a.softcap;
     float slope = 0.0f;
     if (MOD && a.slopes) slope = a.slopes[br * H + h] * kLog2e;
     const float unit = MOD ? 1.0f : p.scale * kLog2e;
     const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};
 
-    // ---- tiles on their way: K straight from memory into LDS, V through registers, where it is looked through for values that
-    // are no finite numbers.  A tile's rows are read through a descriptor that ends where the sequence does: rows
-    // behind it are zeros, and what a lane adds to the tile's address does not change from tile to tile.
+    // ---- tiles on their way, straight from memory into LDS, two tiles ahead.  A tile's rows are read through a descriptor
+    // that ends where the sequence does: rows behind it are zeros, and what a lane adds to the tile's address does not change
+    // from tile to tile.
     const unsigned k_row = (unsigned)H * D * 4, v_row = (unsigned)H * D * 2;
     auto rows_of = [&](const _Float16 *base, unsigned row_bytes, int key0) {
-        return make_rsrc(reinterpret_cast<const char *>(base) + (size_t)(k0 + key0) * row_bytes, (unsigned)min(nk - key0, S::kKeys) * row_bytes);
+        return rsrc_words(reinterpret_cast<const char *>(base) + (size_t)(k0 + key0) * row_bytes, (unsigned)min(nk - key0, S::kKeys) * row_bytes);
     };
     // KiB i * kWaves + w of a tile, 64 chunks, is the wavefront's; further ones are a constant number of rows (or the other K) on
-    const int chunk = w * 64 + l, v_lds = chunk / C * D + v_swap<C>(chunk / C, chunk % C) * 8;
+    const unsigned lds_at = (unsigned)reinterpret_cast<uintptr_t>((lds_ptr_t)lds);
+    const int chunk = w * 64 + l;
     const int k_in = chunk % (S::kKeys * C);
     const unsigned k_off = (unsigned)(k_in / C) * k_row + (unsigned)((chunk / (S::kKeys * C) * H + h) * D + k_swap<C>(k_in / C, k_in % C) * 8) * 2;
-    const unsigned v_off = (unsigned)(chunk / C) * v_row + (unsigned)(h * D + chunk % C * 8) * 2;
-    v4u vr[VP];
-    int doc_r = 0;
+    const unsigned v_off = (unsigned)(chunk / C) * v_row + (unsigned)(h * D + v_swap<C>(chunk / C, chunk % C) * 8) * 2;
+    const bool has_k = KI >= kWaves || w < KI, has_v = VI >= kWaves || w < VI;
     auto request = [&](int tile, int buf) {
-        const rsrc_t r = rows_of(a.k, k_row, tile * S::kKeys);
-        _Float16 *kb = lds + buf * S::kHalves;
-        if (KI >= kWaves || w < KI) {
+        const unsigned kb = lds_at + buf * S::kHalves * 2 + w * 1024, vb = kb + 4 * S::kK;
+        if (has_k) {
+            const v4u r = rows_of(a.k, k_row, tile * S::kKeys);
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
                 constexpr int HALF = KI / 2;
                 const unsigned more = (unsigned)(i * kWaves % HALF * 64 / C) * k_row + (unsigned)(i * kWaves / HALF * H * D) * 2;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(kb + (i * kWaves + w) * 512), 16, (int)k_off, (int)more, 0, 0);
+                load_to_lds(r, kb + i * kWaves * 1024, k_off, more);
             }
         }
-        const rsrc_t rv = rows_of(a.v, v_row, tile * S::kKeys);
-        if (VI >= kWaves || w < VI) {
+        if (has_v) {
+            const v4u r = rows_of(a.v, v_row, tile * S::kKeys);
 #pragma unroll
             for (int i = 0; i < VP; ++i)
-                vr[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rv, (int)v_off, (int)((unsigned)(i * kWaves * 64 / C) * v_row), 0));
-        }
-        if (a.doc_k && tid < S::kKeys) {
-            const int key = tile * S::kKeys + tid;
-            doc_r = key < nk ? a.doc_k[k0 + key] : -1;
+                load_to_lds(r, vb + i * kWaves * 1024, v_off, (unsigned)(i * kWaves * 64 / C) * v_row);
         }
     };
-    auto deposit = [&](int tile, int buf) {
-        _Float16 *vb = lds + buf * S::kHalves + 2 * S::kK;
-        if (VI >= kWaves || w < VI) {
+    // The wavefront's part of a tile has landed (`behind`: one more tile has been requested since).  It looks its V through:
+    // values that are no finite numbers become zeros there, and the tile is marked.
+    auto settle = [&](int tile, int buf, bool behind) {
+        if (behind && has_v) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KP + VP) : "memory");      // (who has V has K)
+        else if (behind && has_k) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KP) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (has_v) {
+            v4u *mine = reinterpret_cast<v4u *>(lds + buf * S::kHalves + 2 * S::kK) + w * 64 + l;
 #pragma unroll
             for (int i = 0; i < VP; ++i) {
+                v4u v = mine[i * kWaves * 64];
                 v2h x = {(_Float16)0.0f, (_Float16)0.0f};           // 0 * v: what is no finite number leaves a NaN
                 const v2h zero = x;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (uint32_t)vr[i][j]), zero, x);
+                for (int j = 0; j < 4; ++j) x = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (uint32_t)v[j]), zero, x);
                 if ((__builtin_bit_cast(uint32_t, x) & 0x7fff7fffu) != 0) {
                     odd_s[buf] = tile;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        uint32_t y = vr[i][j];
+                        uint32_t y = v[j];
                         if ((y & 0x7c00u) == 0x7c00u) y &= 0xffff0000u;
                         if ((y & 0x7c000000u) == 0x7c000000u) y &= 0x0000ffffu;
-                        vr[i][j] = y;
+                        v[j] = y;
                     }
+                    mine[i * kWaves * 64] = v;
                 }
-                *reinterpret_cast<v4u *>(vb + v_lds + i * kWaves * 64 / C * D) = vr[i];
             }
         }
-        if (a.doc_k && tid < S::kKeys) doc_s[buf][tid] = doc_r;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // K lies in LDS
+        if (a.doc_k && tid < S::kKeys) {
+            const int key = tile * S::kKeys + tid;
+            doc_s[buf][tid] = key < nk ? a.doc_k[k0 + key] : -1;
+        }
     };
 
     float m = -INFINITY, sum = 0.0f;
@@ -428,24 +449,26 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             if (!visit) continue;
         }
         const int stop = a.doc_k ? min(from + 64, tiles) : tiles;
-        int tile = a.doc_k ? from + (int)__builtin_ctzll(visit) : 0, buf = 0;
+        auto after = [&](int t) {                       // the tile that follows, or `stop`
+            if (!a.doc_k) return min(t + 1, stop);
+            const unsigned long long rest = t - from >= 63 ? 0 : visit >> (t - from + 1) << (t - from + 1);
+            return rest ? from + (int)__builtin_ctzll(rest) : stop;
+        };
+        int tile = a.doc_k ? from + (int)__builtin_ctzll(visit) : 0, next = after(tile), buf = 0;
         request(tile, 0);
-        deposit(tile, 0);
+        if (next < stop) request(next, 1);
+        settle(tile, 0, next < stop);
         __syncthreads();
         auto step = [&](auto masked) {
-            int next = tile + 1;
-            bool same = false;
-            if (a.doc_k) {
-                same = (uniform >> (tile - from)) & 1;
-                visit &= visit - 1;
-                next = visit ? from + (int)__builtin_ctzll(visit) : stop;
-            }
-            if (next < stop) request(next, buf ^ 1);
+            const int third = next < stop ? after(next) : stop, ahead = buf == 2 ? 0 : buf + 1;
+            if (third < stop) request(third, buf == 0 ? 2 : buf - 1);           // (where the tile before this one was)
+            const bool same = a.doc_k && ((uniform >> (tile - from)) & 1);
             if (!decltype(masked)::value || tile * S::kKeys + sub0 * 32 < most) compute(masked, tile, buf, same);
-            buf ^= 1;
-            if (next < stop) deposit(next, buf);
+            if (next < stop) settle(next, ahead, third < stop);
             __syncthreads();
+            buf = ahead;
             tile = next;
+            next = third;
         };
         // (a loop for the tiles that every row sees whole, and one for the others: what differs between them inside one loop costs
         // copies of the accumulators)
