@@ -3,12 +3,12 @@
 //   out = (softmax(s1) V - lambda softmax(s2) V) / 2, both branches in one pass over the keys with running maxima and sums.
 //
 // A workgroup of eight wavefronts holds 128 query rows of one head and sequence, a wavefront 32 of them for one of the branches, and
-// takes the keys 64 at a time: K1, K2 and V of the tile in LDS, double buffered, requested a tile ahead.  All
+// takes the keys 64 at a time: K1, K2 and V of a tile go straight into LDS, three tiles at a time, requested two ahead.  All
 // products are computed transposed, S^T = K Q^T and O^T = V^T P^T on the 32x32x16 fp16 matrix instruction, so that
 // a lane owns one query: its maximum, sum and rescaling are registers of the lane (one exchange between the halves of the
 // wavefront), and the 8 weights of a step that a lane holds after S^T are the ones it has to supply for O^T if V's
 // keys are taken in the order in which the accumulator's rows lie (4 h .. 4 h + 3 and 8 + 4 h .. for half h): P never
-// moves.  V is transposed on its way into LDS.
+// moves.  V is transposed by the LDS reads that fetch it.
 // Few rows would leave most of the chip idle: then (SPLIT) a workgroup holds 32 rows, takes 128 keys at a time, and its
 // wavefronts share the keys of a tile; they are merged at the end.
 // Weights are relative to the running maximum in base 2 and carried 2^7 larger, so that fp16 holds them down to
@@ -18,8 +18,12 @@
 // given, both only in tiles that need them; tiles whose document numbers lie outside those of the rows are not
 // read.  What a row does not see has weight 0; values of V that are no finite numbers are taken out of the tile and
 // added to the rows that see them (0 * inf would reach the others).
-// Bound by the exponentials and the vector instructions around them up to 64 columns: 32 scores per lane and
-// tile against 16 matrix instructions.
+// What a tile of 64 keys costs a compute unit (64 columns, 32 heads, 4096 rows without causality: 1.4 us): 1024 clocks of
+// matrix instructions, about as many of vector instructions per pair of wavefronts (exponentials 8 clocks, maxima, conversions and
+// dot products 4, the rest 2.5), LDS reads and the barrier.  They add up rather than overlap, with two wavefronts on a SIMD
+// as with four, with the branches' phases set against each other and with the next tile's scores computed during
+// the exponentials (measured: 1.4 to 1.5 all of them), and the clock falls to 1.9 GHz under this load (1.5 under random matrix products
+// alone): 770 TFLOP/s, 860 with 128 columns, against 1350 of a plain matrix product of 8192.
 #include "hgf_kv8.h"
 
 #include <limits.h>
@@ -50,7 +54,8 @@ template <int D, int SPLIT>
 struct Shape {
     static constexpr int kRows = 128 / SPLIT, kGroups = 4 / SPLIT;         // rows, and groups of 32 of them
     static constexpr int kKeys = SPLIT == 1 ? 64 : 32 * SPLIT;
-    static constexpr int kSub = kKeys / 32 / SPLIT;             // groups of 32 keys per wavefront and tile
+    static constexpr int kSub = kKeys / 32 / SPLIT;             // groups of 32 keys per wavefront and tile, and of them worked on
+    static constexpr int kStep = D == 64 ? 1 : kSub;            // together (64 columns: two at a time leave room for half the wavefronts)
     static constexpr int kChunks = D / 8;                       // 16-byte chunks of a row of K or V
     static constexpr int kK = kKeys * D, kHalves = 3 * kK;      // a tile: K1, K2, V
     static constexpr int kTileT = (D + 31) / 32;                // row tiles of O^T
@@ -99,7 +104,7 @@ template <int D, bool MOD, int SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams p)
 {
     using S = Shape<D, SPLIT>;
-    constexpr int KS = D / 16, DT = S::kTileT, SUB = S::kSub, C = S::kChunks;
+    constexpr int KS = D / 16, DT = S::kTileT, SUB = S::kStep, C = S::kChunks;
     constexpr int KI = 2 * S::kKeys * C / 64, VI = S::kKeys * C / 64;           // KiB of K1 and K2, and of V, in a tile
     constexpr int KP = KI > kWaves ? KI / kWaves : 1, VP = VI > kWaves ? VI / kWaves : 1;       // of them per wavefront
     extern __shared__ __align__(16) _Float16 lds[];
@@ -253,24 +258,22 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
-    const int sub0 = split * SUB;                   // the wavefront's groups of 32 keys in a tile
     // its operands' places in LDS: of K for chunk 2 st + half (another eight chunks are 128 bytes further on, 32 rows
     // are a constant too); of V for the even and odd row tiles of O^T, where lane j of 16 asks for 4 columns of key j / 4, and gets
     // 4 keys of column j
     constexpr int KA = KS < 4 ? KS : 4;
     int k_at[KA], v_at[2];
 #pragma unroll
-    for (int st = 0; st < KA; ++st) k_at[st] = br * S::kK + (sub0 * 32 + col) * D + k_swap<C>(col, st * 2 + half) * 8;
+    for (int st = 0; st < KA; ++st) k_at[st] = br * S::kK + col * D + k_swap<C>(col, st * 2 + half) * 8;
     {
         const int key = 4 * half + (l >> 2 & 3), c4 = D < 32 ? l & 3 : (l >> 4 & 1) * 4 + (l & 3);  // quad of columns
 #pragma unroll
-        for (int par = 0; par < 2; ++par) v_at[par] = (sub0 * 32 + key) * D + v_swap<C>(key, (D < 64 ? 0 : par * 4) + c4 / 2) * 8 + (c4 & 1) * 4;
+        for (int par = 0; par < 2; ++par) v_at[par] = key * D + v_swap<C>(key, (D < 64 ? 0 : par * 4) + c4 / 2) * 8 + (c4 & 1) * 4;
     }
     typedef short v4s __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) v4s *lds_v4s_t;
 
-    auto scores = [&](int buf, v16f (&x)[SUB]) {
-        const _Float16 *kb = lds + buf * S::kHalves;
+    auto scores = [&](const _Float16 *kb, v16f (&x)[SUB]) {
         constexpr int KB = D == 128 ? 1 : SUB;          // groups of 32 keys whose operands are requested together
 #pragma unroll
         for (int k1 = 0; k1 < SUB; k1 += KB) {
@@ -289,13 +292,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             }
         }
     };
-    // One tile.  MASKED: some row may not see some key.
-    auto compute = [&](auto masked, int tile, int buf, bool same) {
+    // The keys of a tile from group sub0 on.  MASKED: some row may not see some key.
+    auto compute = [&](auto masked, int tile, int sub0, int buf, bool same, int odd_tile) {
         constexpr bool MASKED = decltype(masked)::value;
         const int key0 = tile * S::kKeys + sub0 * 32;
-        _Float16 *vb = lds + buf * S::kHalves + 2 * S::kK;
+        _Float16 *kb = lds + buf * S::kHalves + sub0 * 32 * D, *vb = kb + 2 * S::kK;
         v16f s[SUB];
-        scores(buf, s);
+        scores(kb, s);
         // in base 2 from here on: s * unit
         if (MOD) {
             if (cap > 0.0f) {
@@ -402,7 +405,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 #pragma unroll
                 for (int t = 0; t < VB; ++t) o[t1 + t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vx[t][st], pr[st], o[t1 + t], 0, 0, 0);
         }
-        if (__builtin_amdgcn_readfirstlane(odd_s[buf]) == tile) {
+        if (odd_tile == tile) {
             // values that are no finite numbers, to the rows that see them
             const int n = min(SUB * 32, nk - key0);
             for (int j = 0; j < n; ++j) {
@@ -463,7 +466,12 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             const int third = next < stop ? after(next) : stop, ahead = buf == 2 ? 0 : buf + 1;
             if (third < stop) request(third, buf == 0 ? 2 : buf - 1);           // (where the tile before this one was)
             const bool same = a.doc_k && ((uniform >> (tile - from)) & 1);
-            if (!decltype(masked)::value || tile * S::kKeys + sub0 * 32 < most) compute(masked, tile, buf, same);
+            const int odd_tile = __builtin_amdgcn_readfirstlane(odd_s[buf]);
+#pragma unroll
+            for (int i = 0; i < S::kSub; i += SUB) {
+                const int sub0 = split * S::kSub + i;
+                if (!decltype(masked)::value || tile * S::kKeys + sub0 * 32 < most) compute(masked, tile, sub0, buf, same, odd_tile);
+            }
             if (next < stop) settle(next, ahead, third < stop);
             __syncthreads();
             buf = ahead;
@@ -545,9 +553,13 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
     p.a = a;
     p.scale = 1.0f / sqrtf((float)d_h);
     const bool mod = a.softcap > 0.0f || a.slopes;
-    // fewer workgroups of 128 rows than the chip holds at a time: 32 rows each (128 columns, for whose tiles of 128 keys LDS has no
-    // room twice: 64 rows)
-    const bool few = (long long)(a.Tq / 128 + a.B) * a.n_heads < 512;
+    // Few workgroups of 128 rows: 32 rows each instead (128 columns, for whose tiles of 128 keys LDS has no room three
+    // times: 64).  It is the faster one up to about 256 workgroups of 128 rows, one to a compute unit, and with 64 columns up
+    // to somewhat fewer.  (us, 128 rows / few, causal: 1000 rows of 32 heads of 32 columns 21.8 / 21.0, 2000 of 16 37.7 / 30.5, of 32
+    // 48 / 58; 64 columns, 1000 rows of 16 heads 27.3 / 20.4, of 32 28.6 / 38.7; 128 columns, 2000 of 16 77 / 69, of 32 98 / 132;
+    // 500 rows of 8 heads of 32, 64, 128 columns 12.8 / 8.1, 16.5 / 10.1, 24.6 / 20.1.  Rows behind many earlier keys all see
+    // about as many, which leaves smaller pieces less to level out: 1900 rows and 7600 keys, 16 heads of 128, 177 / 197.)
+    const bool few = (long long)(a.Tq / 128 + a.B) * a.n_heads < (d_h == 64 || a.Tk / 2 > a.Tq ? 200 : 300);
     hipError_t e = hipSuccess;
     auto go = [&](auto d, auto m, auto split) {
         constexpr int D = decltype(d)::value, SPLIT = decltype(split)::value;
