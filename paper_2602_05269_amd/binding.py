@@ -373,52 +373,45 @@ def hgf_diff_attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
 
 # --------------------------------------------------------------------------- attention over prompts, the paged 8-bit cache
 #
-# These calls take tensors of one device, which is made the current one for the call, and by default that
-# device's current stream.  What they allocate for the caller belongs to the call's stream.
+# These calls take tensors of one GPU, which is the current one during the call, and by default that GPU's
+# current stream.  What they allocate for the caller belongs to the call's stream.
 
-def _at(device, stream):
-    return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
-
-
-def _on(device, call, where: str, *args, stream=None) -> None:
-    if stream is not None and stream.device != device:
-        raise ValueError(f"a stream of {stream.device} for tensors of {device}")
-    with torch.cuda.device(device):
-        _check(call(*args, _stream(stream)), where)
-
-
-def _same_device(device, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors of {t.device} and {device} in one call")
+def _call(gpu: int, stream, where: str, call, *args) -> None:
+    if stream is None:
+        stream = torch.cuda.current_stream(gpu)
+    elif stream.device_index != gpu:
+        raise ValueError(f"{where}: a stream of GPU {stream.device_index} for tensors of GPU {gpu}")
+    if torch.cuda.current_device() == gpu:
+        status = call(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(gpu):
+            status = call(*args, stream.cuda_stream)
+    if status != HGF_OK:
+        raise HgfError(status, where)
 
 
-def _new_ints(device, stream, *shape: int) -> torch.Tensor:
-    with _at(device, stream):
-        return torch.empty(shape, dtype=torch.int32, device=device)
+def _need(t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], gpu: int, name: str) -> int:
+    """The tensor's address, if it is what the call takes."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != gpu or gpu < 0 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} of the call's GPU, not {t.dtype} "
+                         f"{list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _ints(t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str) -> Optional[torch.Tensor]:
-    if t is not None:
-        _dev(t, torch.int32, name)
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be {list(shape)}")
-    return t
+def _may(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], gpu: int, name: str) -> Optional[int]:
+    return None if t is None else _need(t, dtype, shape, gpu, name)
 
 
-def _halves(t: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
-    _dev(t, torch.float16, name)
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be {list(shape)}")
-    return t
+def _new(gpu: int, stream, dtype: torch.dtype, *shape: int, make=torch.empty) -> torch.Tensor:
+    if gpu < 0:
+        raise ValueError("the call's tensors must be in device memory")
+    if stream is None:
+        return make(shape, dtype=dtype, device=gpu)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=gpu)
 
 
-def _slopes(t: Optional[torch.Tensor], n_heads: int) -> Optional[torch.Tensor]:
-    if t is not None:
-        _dev(t, torch.float32, "slopes")
-        if tuple(t.shape) != (2 * n_heads,):
-            raise ValueError("slopes must be [2H]")
-    return t
+_I32, _F16, _F32 = torch.int32, torch.float16, torch.float32
 
 
 def hgf_diff_attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, lam: float,
@@ -432,25 +425,21 @@ def hgf_diff_attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
     key.  prefix int32 [B]: keys that every row sees; doc_q, doc_k int32: document numbers (negative: padding);
     softcap: scores become softcap tanh(score / softcap); slopes fp32 [2H]: minus slope times the distance.  Without
     `out`, rows that belong to no sequence come back as zero."""
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        _dev(t, torch.float16, n)
-    if q.dim() != 3 or v.dim() != 3 or q.shape[1] != 2 * v.shape[1] or q.shape[2] != v.shape[2]:
-        raise ValueError("shapes: q [Tq, 2H, d_h], k [Tk, 2H, d_h], v [Tk, H, d_h]")
-    Tq, H2, d_h = q.shape
-    Tk, H = v.shape[:2]
-    _halves(k, (Tk, H2, d_h), "k")
-    _dev(cu_q, torch.int32, "cu_q")
-    B = cu_q.numel() - 1
-    _ints(cu_q, (B + 1,), "cu_q"), _ints(cu_k, (B + 1,), "cu_k"), _ints(prefix, (B,), "prefix")
-    _ints(doc_q, (Tq,), "doc_q"), _ints(doc_k, (Tk,), "doc_k"), _slopes(slopes, H)
+    gpu = q.get_device()
+    if q.dim() != 3 or v.dim() != 3 or cu_q.dim() != 1:
+        raise ValueError("shapes: q [Tq, 2H, d_h], k [Tk, 2H, d_h], v [Tk, H, d_h], cu_q [B + 1]")
+    Tq, _, d_h = q.shape
+    Tk, H, _ = v.shape
+    B = cu_q.shape[0] - 1
     if out is None:
-        with _at(q.device, stream):
-            out = torch.zeros((Tq, H, d_h), dtype=torch.float16, device=q.device)
-    _halves(out, (Tq, H, d_h), "out")
-    _same_device(q.device, k, v, cu_q, cu_k, prefix, doc_q, doc_k, slopes, out)
-    _on(q.device, lib().hgf_diff_attention_prefill, "hgf_diff_attention_prefill", q.data_ptr(), k.data_ptr(), v.data_ptr(),
-        cu_q.data_ptr(), _ptr(cu_k), B, Tq, Tk, H, d_h, float(lam), 1 if causal else 0, _ptr(prefix), _ptr(doc_q),
-        _ptr(doc_k), float(softcap), _ptr(slopes), out.data_ptr(), stream=stream)
+        out = _new(gpu, stream, _F16, Tq, H, d_h, make=torch.zeros)
+    _call(gpu, stream, "hgf_diff_attention_prefill", lib().hgf_diff_attention_prefill,
+          _need(q, _F16, (Tq, 2 * H, d_h), gpu, "q"), _need(k, _F16, (Tk, 2 * H, d_h), gpu, "k"),
+          _need(v, _F16, (Tk, H, d_h), gpu, "v"), _need(cu_q, _I32, (B + 1,), gpu, "cu_q"),
+          _may(cu_k, _I32, (B + 1,), gpu, "cu_k"), B, Tq, Tk, H, d_h, lam, 1 if causal else 0,
+          _may(prefix, _I32, (B,), gpu, "prefix"), _may(doc_q, _I32, (Tq,), gpu, "doc_q"),
+          _may(doc_k, _I32, (Tk,), gpu, "doc_k"), softcap, _may(slopes, _F32, (2 * H,), gpu, "slopes"),
+          _need(out, _F16, (Tq, H, d_h), gpu, "out"))
     return out
 
 
@@ -462,9 +451,10 @@ class Kv8Pages:
         self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
         self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
         self.n_pages, self.page, self.n_seqs, self.max_pages = n_pages, page, n_seqs, max_pages
-        self.device = self.table.device
+        self.gpu = self.table.get_device()
         self.c = hgf_kv8_pages(n_pages, page, n_seqs, max_pages, self.table.data_ptr(), self.lens.data_ptr(),
                                self.refs.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
 
 class Kv8Cache:
@@ -479,9 +469,10 @@ class Kv8Cache:
         self.k_scale = torch.zeros((n_pages, 2 * n_heads, blocks), dtype=torch.float32, device=device)
         self.v_scale = torch.zeros((n_pages, n_heads, blocks), dtype=torch.float32, device=device)
         self.n_pages, self.page, self.n_heads, self.d_h = n_pages, page, n_heads, d_h
-        self.device = self.k_codes.device
+        self.gpu = self.k_codes.get_device()
         self.c = hgf_kv8_cache(n_pages, page, n_heads, d_h, self.k_codes.data_ptr(), self.k_scale.data_ptr(),
                                self.v_codes.data_ptr(), self.v_scale.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
     def load(self, k_codes: torch.Tensor, k_scale: torch.Tensor, v_codes: torch.Tensor, v_scale: torch.Tensor) -> None:
         """Fills the pool from int8 codes [n_pages, page / 16, heads, 16, d_h] and fp32 scales [n_pages, page / 16, heads]."""
@@ -492,92 +483,87 @@ class Kv8Cache:
         self.v_scale.copy_(v_scale.transpose(1, 2))
 
 
+def _pages_of(cache: Kv8Cache, pages: Kv8Pages):
+    if pages.gpu != cache.gpu:
+        raise ValueError("the cache and its pages lie on two devices")
+    return pages.ref
+
+
 def hgf_kv8_pages_grow(pages: Kv8Pages, seqs: torch.Tensor, new: torch.Tensor, ok: Optional[torch.Tensor] = None,
                        stream=None) -> torch.Tensor:
     """Sequences seqs (int32 [n]) become new (int32 [n]) positions longer -> int32 [n]: 1, or 0 where refused."""
-    n = seqs.numel()
+    n, gpu = seqs.numel(), pages.gpu
     if ok is None:
-        ok = _new_ints(pages.device, stream, n)
-    _ints(seqs, (n,), "seqs"), _ints(new, (n,), "new"), _ints(ok, (n,), "ok")
-    _same_device(pages.device, seqs, new, ok)
-    _on(pages.device, lib().hgf_kv8_pages_grow, "hgf_kv8_pages_grow", ctypes.byref(pages.c), seqs.data_ptr(), new.data_ptr(),
-        n, ok.data_ptr(), stream=stream)
+        ok = _new(gpu, stream, _I32, n)
+    _call(gpu, stream, "hgf_kv8_pages_grow", lib().hgf_kv8_pages_grow, pages.ref, _need(seqs, _I32, (n,), gpu, "seqs"),
+          _need(new, _I32, (n,), gpu, "new"), n, _need(ok, _I32, (n,), gpu, "ok"))
     return ok
 
 
 def hgf_kv8_pages_fork(pages: Kv8Pages, src: torch.Tensor, dst: torch.Tensor, pairs: Optional[torch.Tensor] = None,
                        ok: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The empty sequences dst become what src are -> (pairs of pages to copy in every cache int32 [n, 2], ok int32 [n])."""
-    n = src.numel()
-    pairs = _new_ints(pages.device, stream, n, 2) if pairs is None else pairs
-    ok = _new_ints(pages.device, stream, n) if ok is None else ok
-    _ints(src, (n,), "src"), _ints(dst, (n,), "dst"), _ints(pairs, (n, 2), "pairs"), _ints(ok, (n,), "ok")
-    _same_device(pages.device, src, dst, pairs, ok)
-    _on(pages.device, lib().hgf_kv8_pages_fork, "hgf_kv8_pages_fork", ctypes.byref(pages.c), src.data_ptr(), dst.data_ptr(), n,
-        pairs.data_ptr(), ok.data_ptr(), stream=stream)
+    n, gpu = src.numel(), pages.gpu
+    if pairs is None:
+        pairs = _new(gpu, stream, _I32, n, 2)
+    if ok is None:
+        ok = _new(gpu, stream, _I32, n)
+    _call(gpu, stream, "hgf_kv8_pages_fork", lib().hgf_kv8_pages_fork, pages.ref, _need(src, _I32, (n,), gpu, "src"),
+          _need(dst, _I32, (n,), gpu, "dst"), n, _need(pairs, _I32, (n, 2), gpu, "pairs"), _need(ok, _I32, (n,), gpu, "ok"))
     return pairs, ok
 
 
 def hgf_kv8_pages_free(pages: Kv8Pages, seqs: torch.Tensor, stream=None) -> None:
     """The sequences become empty; pages that no sequence has any more are free."""
-    n = seqs.numel()
-    _ints(seqs, (n,), "seqs")
-    _same_device(pages.device, seqs)
-    _on(pages.device, lib().hgf_kv8_pages_free, "hgf_kv8_pages_free", ctypes.byref(pages.c), seqs.data_ptr(), n, stream=stream)
+    n, gpu = seqs.numel(), pages.gpu
+    _call(gpu, stream, "hgf_kv8_pages_free", lib().hgf_kv8_pages_free, pages.ref, _need(seqs, _I32, (n,), gpu, "seqs"), n)
 
 
 def hgf_kv8_pages_compact(pages: Kv8Pages, pairs: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
                           moved: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """The pages in use get the lowest numbers -> (pairs int32 [max(1, n_pages / 2), 2] to copy in every cache, their
     number int32 [1], the new number of every page int32 [n_pages])."""
-    room = max(1, pages.n_pages // 2)
-    pairs = _new_ints(pages.device, stream, room, 2) if pairs is None else pairs
-    count = _new_ints(pages.device, stream, 1) if count is None else count
-    moved = _new_ints(pages.device, stream, pages.n_pages) if moved is None else moved
-    _ints(pairs, (room, 2), "pairs"), _ints(count, (1,), "count"), _ints(moved, (pages.n_pages,), "moved")
-    _same_device(pages.device, pairs, count, moved)
-    _on(pages.device, lib().hgf_kv8_pages_compact, "hgf_kv8_pages_compact", ctypes.byref(pages.c), pairs.data_ptr(),
-        count.data_ptr(), moved.data_ptr(), stream=stream)
+    room, gpu = max(1, pages.n_pages // 2), pages.gpu
+    pairs = _new(gpu, stream, _I32, room, 2) if pairs is None else pairs
+    count = _new(gpu, stream, _I32, 1) if count is None else count
+    moved = _new(gpu, stream, _I32, pages.n_pages) if moved is None else moved
+    _call(gpu, stream, "hgf_kv8_pages_compact", lib().hgf_kv8_pages_compact, pages.ref,
+          _need(pairs, _I32, (room, 2), gpu, "pairs"), _need(count, _I32, (1,), gpu, "count"),
+          _need(moved, _I32, (pages.n_pages,), gpu, "moved"))
     return pairs, count, moved
 
 
 def hgf_kv8_copy_pages(cache: Kv8Cache, pairs: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None) -> None:
     """Copies page pairs[i][0] of the cache to page pairs[i][1]; with count (int32 [1]) the first so many."""
-    n = pairs.shape[0]
-    _ints(pairs, (n, 2), "pairs"), _ints(count, (1,), "count")
-    _same_device(cache.device, pairs, count)
-    _on(cache.device, lib().hgf_kv8_copy_pages, "hgf_kv8_copy_pages", ctypes.byref(cache.c), pairs.data_ptr(), _ptr(count), n,
-        stream=stream)
+    n, gpu = pairs.shape[0], cache.gpu
+    _call(gpu, stream, "hgf_kv8_copy_pages", lib().hgf_kv8_copy_pages, cache.ref, _need(pairs, _I32, (n, 2), gpu, "pairs"),
+          _may(count, _I32, (1,), gpu, "count"), n)
 
 
 def hgf_kv8_append(k: torch.Tensor, v: torch.Tensor, cache: Kv8Cache, pages: Kv8Pages, cu_new: Optional[torch.Tensor] = None,
                    seqs: Optional[torch.Tensor] = None, stream=None) -> None:
     """Writes new tokens, k fp16 [T, 2H, d_h] and v [T, H, d_h], as the last positions of their sequences: row b of the batch
     is sequence seqs[b] (None: b) and has rows cu_new[b] .. cu_new[b+1]-1 (int32 [B + 1]; None: one each)."""
-    T = v.shape[0]
-    _halves(k, (T, 2 * cache.n_heads, cache.d_h), "k"), _halves(v, (T, cache.n_heads, cache.d_h), "v")
+    T, H, d_h, gpu = v.shape[0], cache.n_heads, cache.d_h, cache.gpu
     B = cu_new.numel() - 1 if cu_new is not None else T
-    _ints(cu_new, (B + 1,), "cu_new"), _ints(seqs, (B,), "seqs")
-    _same_device(cache.device, k, v, pages.table, cu_new, seqs)
-    _on(cache.device, lib().hgf_kv8_append, "hgf_kv8_append", k.data_ptr(), v.data_ptr(), ctypes.byref(cache.c),
-        ctypes.byref(pages.c), _ptr(seqs), _ptr(cu_new), B, T, stream=stream)
+    _call(gpu, stream, "hgf_kv8_append", lib().hgf_kv8_append, _need(k, _F16, (T, 2 * H, d_h), gpu, "k"),
+          _need(v, _F16, (T, H, d_h), gpu, "v"), cache.ref, _pages_of(cache, pages), _may(seqs, _I32, (B,), gpu, "seqs"),
+          _may(cu_new, _I32, (B + 1,), gpu, "cu_new"), B, T)
 
 
 def hgf_kv8_gather(cache: Kv8Cache, pages: Kv8Pages, cu: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                    seqs: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The last cu[b+1] - cu[b] positions of row b's sequence as fp16, into rows cu[b] .. of k [T, 2H, d_h] and v [T, H, d_h]."""
-    T = v.shape[0]
-    _halves(k, (T, 2 * cache.n_heads, cache.d_h), "k"), _halves(v, (T, cache.n_heads, cache.d_h), "v")
+    T, H, d_h, gpu = v.shape[0], cache.n_heads, cache.d_h, cache.gpu
     B = cu.numel() - 1
-    _ints(cu, (B + 1,), "cu"), _ints(seqs, (B,), "seqs")
-    _same_device(cache.device, k, v, pages.table, cu, seqs)
-    _on(cache.device, lib().hgf_kv8_gather, "hgf_kv8_gather", ctypes.byref(cache.c), ctypes.byref(pages.c), _ptr(seqs),
-        cu.data_ptr(), B, T, k.data_ptr(), v.data_ptr(), stream=stream)
+    _call(gpu, stream, "hgf_kv8_gather", lib().hgf_kv8_gather, cache.ref, _pages_of(cache, pages),
+          _may(seqs, _I32, (B,), gpu, "seqs"), _need(cu, _I32, (B + 1,), gpu, "cu"), B, T,
+          _need(k, _F16, (T, 2 * H, d_h), gpu, "k"), _need(v, _F16, (T, H, d_h), gpu, "v"))
     return k, v
 
 
 def hgf_diff_attention_kv8_workspace_bytes(B: int, pages: Kv8Pages, n_heads: int, d_h: int) -> int:
-    return lib().hgf_diff_attention_kv8_workspace_bytes(B, ctypes.byref(pages.c), n_heads, d_h)
+    return lib().hgf_diff_attention_kv8_workspace_bytes(B, pages.ref, n_heads, d_h)
 
 
 def hgf_diff_attention_decode_kv8(q: torch.Tensor, cache: Kv8Cache, pages: Kv8Pages, lam: float,
@@ -586,23 +572,17 @@ def hgf_diff_attention_decode_kv8(q: torch.Tensor, cache: Kv8Cache, pages: Kv8Pa
                                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One decode step over the 8-bit cache: q fp16 [B, 2H, d_h], row b of sequence seqs[b] (None: b), whose newest token
     has been appended -> fp16 [B, H, d_h]."""
-    B = q.shape[0]
-    H, d_h = cache.n_heads, cache.d_h
-    _halves(q, (B, 2 * H, d_h), "q")
-    _ints(seqs, (B,), "seqs"), _slopes(slopes, H)
-    need = hgf_diff_attention_kv8_workspace_bytes(B, pages, H, d_h)
-    with _at(cache.device, stream):
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        if out is None:
-            out = torch.empty((B, H, d_h), dtype=torch.float16, device=q.device)
-    _halves(out, (B, H, d_h), "out")
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor in device memory")
-    _same_device(cache.device, q, pages.table, seqs, slopes, out, workspace)
-    _on(cache.device, lib().hgf_diff_attention_decode_kv8, "hgf_diff_attention_decode_kv8", q.data_ptr(),
-        ctypes.byref(cache.c), ctypes.byref(pages.c), _ptr(seqs), B, float(lam), float(softcap), _ptr(slopes), out.data_ptr(),
-        workspace.data_ptr() if need else None, workspace.numel() * workspace.element_size(), stream=stream)
+    B, H, d_h, gpu = q.shape[0], cache.n_heads, cache.d_h, cache.gpu
+    if workspace is None:
+        need = hgf_diff_attention_kv8_workspace_bytes(B, pages, H, d_h)
+        workspace = _new(gpu, stream, torch.uint8, need)
+    if out is None:
+        out = _new(gpu, stream, _F16, B, H, d_h)
+    size = workspace.numel() * workspace.element_size()
+    _call(gpu, stream, "hgf_diff_attention_decode_kv8", lib().hgf_diff_attention_decode_kv8,
+          _need(q, _F16, (B, 2 * H, d_h), gpu, "q"), cache.ref, _pages_of(cache, pages), _may(seqs, _I32, (B,), gpu, "seqs"),
+          B, lam, softcap, _may(slopes, _F32, (2 * H,), gpu, "slopes"), _need(out, _F16, (B, H, d_h), gpu, "out"),
+          _need(workspace, workspace.dtype, workspace.shape, gpu, "workspace") if size else None, size)
     return out
 
 
