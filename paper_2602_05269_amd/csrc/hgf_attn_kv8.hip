@@ -63,17 +63,32 @@ __device__ inline float soft_cap(float x, float cap, float inv)
     return cap * (fabsf(y) < 0.3f ? series : t);
 }
 
-template <int D, bool MOD>
-__global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnParams p)
+template <int D, bool MOD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
 {
     constexpr int LD = D / 16;                      // 16-byte loads per lane of one head of K (or V) for 64 positions
     constexpr int QC = D == 128 ? 2 : 1;            // chunks of 16 columns whose digits a lane holds
-    __shared__ __align__(16) unsigned char dig[4][8][kTile];
-    __shared__ float o_s[4][2][D], m_s[4][2], l_s[4][2];
+    __shared__ __align__(16) unsigned char dig[WAVES][8][kTile];
+    __shared__ float o_s[WAVES][2][D], m_s[WAVES][2], l_s[WAVES][2];
     const KvView &kv = p.kv;
     const int H = kv.n_heads, h = blockIdx.x, part = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, l = tid & 63, g = l >> 4, r = l & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // (q is requested before anything is known of the sequence: fewer trips to memory one after the other)
+    v8h q_raw[2][QC][2];
+    _Float16 q_own[2][LD];
+#pragma unroll
+    for (int br = 0; br < 2; ++br) {
+        const _Float16 *qr = p.q + ((size_t)b * 2 * H + br * H + h) * D;
+#pragma unroll
+        for (int c = 0; c < LD; ++c) q_own[br][c] = qr[c * 16 + r];
+#pragma unroll
+        for (int i = 0; i < QC; ++i) {
+            const v8h *src = reinterpret_cast<const v8h *>(qr + (i * 4 + g % LD) * 16);     // (D < 64: the k-groups repeat the chunks)
+            q_raw[br][i][0] = src[0];
+            q_raw[br][i][1] = src[1];
+        }
+    }
     const int seq = kv.seq(b);
     const int len = seq >= 0 ? kv.len(seq) : 0;
     const int tiles = (len + kTile - 1) / kTile, each = (tiles + p.parts - 1) / p.parts;
@@ -90,11 +105,10 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnParams p)
     bool odd = false;
 #pragma unroll
     for (int br = 0; br < 2; ++br) {
-        const _Float16 *qr = p.q + ((size_t)b * 2 * H + br * H + h) * D;
         float amax = 0.0f;
 #pragma unroll
         for (int c = 0; c < LD; ++c) {
-            const float x = fabsf((float)qr[c * 16 + r]);
+            const float x = fabsf((float)q_own[br][c]);
             odd |= !(x <= 65504.0f);
             amax = x <= 65504.0f ? fmaxf(amax, x) : amax;
         }
@@ -103,11 +117,9 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnParams p)
         q_scale[br] = amax > 0.0f ? reciprocal_of_power(f) * p.scale : 0.0f;
 #pragma unroll
         for (int i = 0; i < QC; ++i) {
-            const int c = i * 4 + g % LD;           // (D < 64: the k-groups repeat the head's chunks)
-            const v8h *src = reinterpret_cast<const v8h *>(qr + c * 16);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const v8h x = src[half];
+                const v8h x = q_raw[br][i][half];
                 uint32_t word[2] = {0, 0};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -134,7 +146,7 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnParams p)
         slope[1] = p.slopes[H + h];
     }
 
-    for (int tile = t0 + w; tile < t1; tile += 4) {
+    for (int tile = t0 + w; tile < t1; tile += WAVES) {
         const int pos = tile * kTile + l;
         const int blk = tile * 4 + g;               // the lane's own block of 16 positions
         const int own = kv.page_of(seq, blk);
@@ -223,10 +235,10 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnParams p)
     float acc = 0.0f, total = 0.0f, top = -INFINITY;
     if (br < 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, m_s[i][br]);
+        for (int i = 0; i < WAVES; ++i) top = fmaxf(top, m_s[i][br]);
         const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < WAVES; ++i) {
             const float f = __builtin_amdgcn_exp2f(m_s[i][br] - base);
             acc += o_s[i][br][d] * f;
             total += l_s[i][br] * f;
@@ -305,9 +317,13 @@ __global__ __launch_bounds__(512) void kv8_merge_kernel(Kv8AttnParams p)
 }
 
 // Parts of every sequence: enough workgroups to fill the chip several times over, none of fewer than 256 positions of
-// the table's capacity.
+// the table's capacity.  Tables of up to 1024 positions are one part, taken by workgroups of eight wavefronts: two
+// tiles a wavefront at most cost less than the merge's launch (24 sequences of up to 512, 8 heads of 32: 7.9 us, in three
+// parts of four wavefronts 8.6 and 3.7).
+constexpr int kOnePart = 1024;
 int parts_of(int B, long long capacity, int n_heads)
 {
+    if (capacity <= kOnePart) return 1;
     const long long most = (capacity + 255) / 256, want = (2048 + (long long)B * n_heads - 1) / ((long long)B * n_heads);
     return (int)(want < 1 ? 1 : want < most ? want : most);
 }
@@ -334,11 +350,13 @@ hipError_t launch_diff_attn_kv8(const void *q, const KvView &kv, int B, int d_h,
     p.softcap = softcap;
     p.scale = 1.0f / sqrtf((float)d_h);
     const dim3 grid(kv.n_heads, p.parts, B);
-    const bool mod = softcap > 0.0f || slopes;
+    const bool mod = softcap > 0.0f || slopes, one = ((long long)kv.max_pages << kv.page_log2) <= kOnePart;
     auto go = [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((kv8_attn_kernel<D, false>), grid, dim3(256), 0, st, p);
+        if (one && mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true, 8>), grid, dim3(512), 0, st, p);
+        else if (one) hipLaunchKernelGGL((kv8_attn_kernel<D, false, 8>), grid, dim3(512), 0, st, p);
+        else if (mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true, 4>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((kv8_attn_kernel<D, false, 4>), grid, dim3(256), 0, st, p);
         if (p.parts > 1) hipLaunchKernelGGL(kv8_merge_kernel<D>, dim3(kv.n_heads, B), dim3(512), 0, st, p);
     };
     switch (d_h) {
