@@ -228,7 +228,7 @@ hgf_status hgf_diff_attention_decode(const void *q_f16, const void *k_cache_f16,
  *   prefix       int32 [B] (device) or NULL: so many keys of the sequence are seen from every row
  *   doc_q, doc_k int32 [Tq], int32 [Tk] (device), both or none: document numbers in any order; negative: padding, which sees
  *                nothing and is not seen
- *   softcap      0 (none) or positive
+ *   softcap      0 (none) or 1e-20 .. 1e20
  *   slopes       fp32 [2 n_heads] (device) or NULL: a distance bias per head of q
  *   out_f16      fp16 [Tq, n_heads, d_h]; rows in front of cu_q[0] and behind cu_q[B] are left as they are
  * d_h 16, 32, 64 or 128; n_heads <= 1024; Tq, Tk < 2^24.  fp32 scores and sums; the softmax weights are

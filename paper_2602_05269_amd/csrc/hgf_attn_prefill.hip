@@ -83,11 +83,17 @@ __device__ inline int opaque(int v)
 // 64 x 16 bytes from memory straight into LDS, in flight until a wait on vmcnt.  (In assembly because with the builtin the compiler
 // waits for everything in flight before the transposing LDS reads, whichever buffer they read.  Nothing comes back in
 // registers, and the kernel's own waits are the only ones that are needed.)
-__device__ inline void load_to_lds(v4u rsrc, unsigned lds_byte, unsigned lane_off, unsigned off)
+__device__ inline void load_to_lds(v4u rsrc, unsigned lds_byte, unsigned lane_off)
 {
     unsigned kept;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
-                 : "=&s"(kept) : "s"(lds_byte), "v"(lane_off), "s"(rsrc), "s"(off) : "memory");
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds_byte), "v"(lane_off), "s"(rsrc) : "memory");
+}
+__device__ inline void load4_to_lds(v4u rsrc, unsigned lds_byte, unsigned lane_off)      // 64 x 4 bytes
+{
+    unsigned kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds_byte), "v"(lane_off), "s"(rsrc) : "memory");
 }
 __device__ inline v4u rsrc_words(const void *base, unsigned bytes)
 {
@@ -139,7 +145,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     const bool counts = real && doc >= 0;
     // the fewest keys that a row of the wavefront sees (0 for padding: its rows see none), and the most
     const int least = -(int)wave_max((float)-(real ? limit : nk)), most = (int)wave_max((float)limit);
-    int tiles, whole, doc_lo = 0, doc_hi = 0;       // tiles that some row sees, that all rows see whole
+    int tiles, whole;                               // tiles that some row sees, that all rows see whole
+    int doc_lo, doc_hi, wave_lo, wave_hi;           // document numbers of all rows, and of the wavefront's
     {
         int lo = counts ? doc : INT_MAX, hi = counts ? doc : -1;
         if (a.doc_q) {
@@ -149,6 +156,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 hi = max(hi, __shfl_xor(hi, o, 64));
             }
         }
+        wave_lo = lo;
+        wave_hi = hi;
         if (tid < 3) odd_s[tid] = -1;
         if (l == 0) {
             most_s[w] = most;
@@ -180,7 +189,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     }
 #pragma unroll
     for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));     // (they are waited for here, not in the loop)
-    const float cap = a.softcap;
+    const float cap = a.softcap, cap_in = cap > 0.0f ? p.scale / cap * (2.0f * kLog2e) : 0.0f, cap_out = cap * kLog2e;
     float slope = 0.0f;
     if (MOD && a.slopes) slope = a.slopes[br * H + h] * kLog2e;
     const float unit = MOD ? 1.0f : p.scale * kLog2e;
@@ -188,7 +197,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 
     // ---- tiles on their way, straight from memory into LDS, two tiles ahead.  A tile's rows are read through a descriptor
     // that ends where the sequence does: rows behind it are zeros, and what a lane adds to the tile's address does not change
-    // from tile to tile.
+    // from tile to tile.  (All of it is in the lane's offset: that is what the descriptor's end is held against.)
     const unsigned k_row = (unsigned)H * D * 4, v_row = (unsigned)H * D * 2;
     auto rows_of = [&](const _Float16 *base, unsigned row_bytes, int key0) {
         return rsrc_words(reinterpret_cast<const char *>(base) + (size_t)(k0 + key0) * row_bytes, (unsigned)min(nk - key0, S::kKeys) * row_bytes);
@@ -199,7 +208,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     const int k_in = chunk % (S::kKeys * C);
     const unsigned k_off = (unsigned)(k_in / C) * k_row + (unsigned)((chunk / (S::kKeys * C) * H + h) * D + k_swap<C>(k_in / C, k_in % C) * 8) * 2;
     const unsigned v_off = (unsigned)(chunk / C) * v_row + (unsigned)(h * D + v_swap<C>(chunk / C, chunk % C) * 8) * 2;
-    const bool has_k = KI >= kWaves || w < KI, has_v = VI >= kWaves || w < VI;
+    const unsigned doc_at = (unsigned)reinterpret_cast<uintptr_t>((lds_ptr_t)doc_s);
+    const bool has_k = KI >= kWaves || w < KI, has_v = VI >= kWaves || w < VI, has_doc = a.doc_k && w < S::kKeys / 64;
+    static_assert(S::kKeys / 64 <= VI && VI <= KI, "who has documents has V, and who has V has K");
     auto request = [&](int tile, int buf) {
         const unsigned kb = lds_at + buf * S::kHalves * 2 + w * 1024, vb = kb + 4 * S::kK;
         if (has_k) {
@@ -208,20 +219,26 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             for (int i = 0; i < KP; ++i) {
                 constexpr int HALF = KI / 2;
                 const unsigned more = (unsigned)(i * kWaves % HALF * 64 / C) * k_row + (unsigned)(i * kWaves / HALF * H * D) * 2;
-                load_to_lds(r, kb + i * kWaves * 1024, k_off, more);
+                load_to_lds(r, kb + i * kWaves * 1024, k_off + more);
             }
         }
         if (has_v) {
             const v4u r = rows_of(a.v, v_row, tile * S::kKeys);
 #pragma unroll
             for (int i = 0; i < VP; ++i)
-                load_to_lds(r, vb + i * kWaves * 1024, v_off, (unsigned)(i * kWaves * 64 / C) * v_row);
+                load_to_lds(r, vb + i * kWaves * 1024, v_off + (unsigned)(i * kWaves * 64 / C) * v_row);
+        }
+        if (has_doc) {                              // (behind the sequence zeros: no row sees those keys)
+            const int key0 = tile * S::kKeys;
+            load4_to_lds(rsrc_words(a.doc_k + k0 + key0, (unsigned)min(nk - key0, S::kKeys) * 4), doc_at + (buf * S::kKeys + w * 64) * 4,
+                         (unsigned)tid * 4);
         }
     };
     // The wavefront's part of a tile has landed (`behind`: one more tile has been requested since).  It looks its V through:
     // values that are no finite numbers become zeros there, and the tile is marked.
     auto settle = [&](int tile, int buf, bool behind) {
-        if (behind && has_v) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KP + VP) : "memory");      // (who has V has K)
+        if (behind && has_doc) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KP + VP + 1) : "memory");
+        else if (behind && has_v) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KP + VP) : "memory");
         else if (behind && has_k) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KP) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (has_v) {
@@ -245,10 +262,6 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                     mine[i * kWaves * 64] = v;
                 }
             }
-        }
-        if (a.doc_k && tid < S::kKeys) {
-            const int key = tile * S::kKeys + tid;
-            doc_s[buf][tid] = key < nk ? a.doc_k[k0 + key] : -1;
         }
     };
 
@@ -302,36 +315,30 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         // in base 2 from here on: s * unit
         if (MOD) {
             if (cap > 0.0f) {
-                const float in = p.scale / cap, out = cap * kLog2e;
+                // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1)
 #pragma unroll
                 for (int kt = 0; kt < SUB; ++kt)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float y = s[kt][e] * in;
-                        const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * kLog2e)) + 1.0f);
+                        const float y = s[kt][e] * cap_in;          // 2 x / cap, in base 2
+                        const float t = __builtin_fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.0f), -2.0f * cap_out, cap_out);
                         if (cap > kCoarseCap) {
-                            const float y2 = y * y;
-                            const float series = y * __builtin_fmaf(y2, __builtin_fmaf(y2, __builtin_fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f),
+                            const float z = y * (0.5f / kLog2e), z2 = z * z;
+                            const float series = z * __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, -17.0f / 315.0f, 2.0f / 15.0f),
                                                                                      -1.0f / 3.0f), 1.0f);
-                            s[kt][e] = (fabsf(y) < 0.3f ? series : t) * out;
+                            s[kt][e] = fabsf(z) < 0.3f ? series * cap_out : t;
                         } else {
-                            s[kt][e] = t * out;
+                            s[kt][e] = t;
                         }
                     }
-            } else {
-#pragma unroll
-                for (int kt = 0; kt < SUB; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[kt][e] *= p.scale * kLog2e;
             }
-            if (a.slopes) {
-                const float away = (float)(pos - key0 - 4 * half);
+            const float by = cap > 0.0f ? 1.0f : p.scale * kLog2e;
+            const float away = (float)(pos - key0 - 4 * half);
 #pragma unroll
-                for (int kt = 0; kt < SUB; ++kt)
+            for (int kt = 0; kt < SUB; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        s[kt][e] = __builtin_fmaf(-slope, fabsf(away - (float)(kt * 32 + 8 * (e >> 2) + (e & 3))), s[kt][e]);
-            }
+                for (int e = 0; e < 16; ++e)                        // (without slopes: slope is 0)
+                    s[kt][e] = __builtin_fmaf(s[kt][e], by, -slope * fabsf(away - (float)(kt * 32 + 8 * (e >> 2) + (e & 3))));
         }
         if (MASKED) {
             const int left = opaque(limit - key0 - 4 * half);
@@ -428,7 +435,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 
     // ---- the keys, in windows: all of them, or 64 tiles at a time of which those are taken whose documents can matter
     for (int from = 0; from < tiles; from += 64) {
-        unsigned long long visit = 0, uniform = 0;
+        unsigned long long visit = 0, mine = 0, uniform = 0;        // tiles of the window: to be read, for this wavefront, of one document
         if (a.doc_k) {
             constexpr int EACH = S::kKeys / kWaves;     // a lane looks at so many keys of tile from + l
             int lo = INT_MAX, hi = INT_MIN;
@@ -447,7 +454,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
                 hi = max(hi, win_hi[i][l]);
             }
             visit = __ballot(from + l < tiles && hi >= doc_lo && lo <= doc_hi);
-            uniform = __ballot(lo == hi && lo == doc_lo && lo == doc_hi);
+            mine = __ballot(hi >= wave_lo && lo <= wave_hi);
+            uniform = __ballot(lo == hi && lo == wave_lo && lo == wave_hi);
             __syncthreads();                            // (the window's arrays are read before the next window's are written)
             if (!visit) continue;
         }
@@ -465,12 +473,12 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         auto step = [&](auto masked) {
             const int third = next < stop ? after(next) : stop, ahead = buf == 2 ? 0 : buf + 1;
             if (third < stop) request(third, buf == 0 ? 2 : buf - 1);           // (where the tile before this one was)
-            const bool same = a.doc_k && ((uniform >> (tile - from)) & 1);
+            const bool same = a.doc_k && ((uniform >> (tile - from)) & 1), skip = a.doc_k && !((mine >> (tile - from)) & 1);
             const int odd_tile = __builtin_amdgcn_readfirstlane(odd_s[buf]);
 #pragma unroll
             for (int i = 0; i < S::kSub; i += SUB) {
                 const int sub0 = split * S::kSub + i;
-                if (!decltype(masked)::value || tile * S::kKeys + sub0 * 32 < most) compute(masked, tile, sub0, buf, same, odd_tile);
+                if (!decltype(masked)::value || (!skip && tile * S::kKeys + sub0 * 32 < most)) compute(masked, tile, sub0, buf, same, odd_tile);
             }
             if (next < stop) settle(next, ahead, third < stop);
             __syncthreads();

@@ -316,8 +316,9 @@ hipError_t launch_kv8_copy_pages(const hgf_kv8_cache &c, const int32_t *pairs, c
     p.n_pages = c.n_pages;
     const int pieces = (int)((p.bytes[0] + kCopyPiece - 1) / kCopyPiece);
     p.splits = pieces < 64 ? pieces : 64;
-    // lists whose count lies on the device may be far longer than what is in them: their workgroups take several pairs
-    const int rows = n < 4096 ? n : 4096;
+    // (lists whose count lies on the device may be far longer than what is in them: not a workgroup for every pair there
+    // could be)
+    const int most = 8192 / p.splits, rows = n < most ? n : most;
     hipLaunchKernelGGL(kv8_copy_kernel, dim3(p.splits, rows), dim3(256), 0, st, p);
     return hipGetLastError();
 }

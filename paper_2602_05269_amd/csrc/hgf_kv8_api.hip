@@ -38,7 +38,7 @@ bool head_ok(int n_heads, int d_h)
     return n_heads >= 1 && n_heads <= kMaxHeads && (d_h == 16 || d_h == 32 || d_h == 64 || d_h == 128);
 }
 bool page_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128 || page == 256; }
-bool cap_ok(float cap) { return cap >= 0.0f && !isinf(cap); }          // (what is not a number is not)
+bool cap_ok(float cap) { return cap == 0.0f || (cap >= 1e-20f && cap <= 1e20f); }      // (what is not a number is not)
 bool number_ok(float v) { return !isnan(v) && !isinf(v); }
 
 hgf_status check_pages(const hgf_kv8_pages *p)

@@ -34,7 +34,7 @@ def test_prefill_refusals():
         assert _prefill(**{name: None}) == 1
     assert _prefill(doc_q=0x600) == 1 and _prefill(doc_k=0x600) == 1
     for bad in (dict(B=0), dict(B=16385), dict(Tq=0), dict(Tk=0), dict(Tq=1 << 24, cu_k=0x700), dict(Tk=9), dict(H=0), dict(H=1025), dict(d=8),
-                dict(d=48), dict(d=256), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(lam=float("nan"))):
+                dict(d=48), dict(d=256), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-21), dict(cap=2e20), dict(lam=float("nan"))):
         assert _prefill(**bad) == 2, bad
     for name in ("q", "k", "v", "out"):
         assert _prefill(**{name: 0x108}) == 3
