@@ -376,16 +376,22 @@ def hgf_diff_attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
 # These calls take tensors of one GPU, which is the current one during the call, and by default that GPU's
 # current stream.  What they allocate for the caller belongs to the call's stream.
 
+# The handle of a GPU's current stream; without the Stream object, which takes a microsecond to make, where torch has that.
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
+
+
 def _call(gpu: int, stream, where: str, call, *args) -> None:
     if stream is None:
-        stream = torch.cuda.current_stream(gpu)
+        handle = _current_handle(gpu)
     elif stream.device_index != gpu:
         raise ValueError(f"{where}: a stream of GPU {stream.device_index} for tensors of GPU {gpu}")
+    else:
+        handle = stream.cuda_stream
     if torch.cuda.current_device() == gpu:
-        status = call(*args, stream.cuda_stream)
+        status = call(*args, handle)
     else:
         with torch.cuda.device(gpu):
-            status = call(*args, stream.cuda_stream)
+            status = call(*args, handle)
     if status != HGF_OK:
         raise HgfError(status, where)
 

@@ -125,9 +125,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 
     // ---- which rows: the slots of sequence b begin at cu_q[b] / kRows + b; the last ones first (they see the most keys)
     const int slot = p.slots - 1 - (int)(blockIdx.x / H);
-    const int b = wave_search(a.B, slot, [&](int x) { return min(max(a.cu_q[x], 0), a.Tq) / S::kRows + x; });
     int q0, nq, k0, nk;
-    clipped_rows(a.cu_q, b, a.Tq, q0, nq);
+    const int b = slot_entry<S::kRows == 128 ? 7 : S::kRows == 64 ? 6 : 5, 1>(a.cu_q, a.B, a.Tq, slot, q0, nq);
     clipped_rows(a.cu_k, b, a.Tk, k0, nk);
     const int first = (slot - q0 / S::kRows - b) * S::kRows;
     if (first < 0 || first >= nq) return;

@@ -64,6 +64,26 @@ __device__ inline int wave_search(int B, int at, Key key)
     return lo;
 }
 
+// Batch entry b that slot `at` of a grid belongs to, where entry b has the slots from row(b) / 2^SHIFT + PER b on (row(b): its first
+// row), and its rows.  Up to 64 entries in one trip to memory.
+template <int SHIFT, int PER>
+__device__ inline int slot_entry(const int32_t *cu, int B, int T, int at, int &first, int &n)
+{
+    auto clip = [&](int x) { return min(max(x, 0), T); };
+    if (B <= 64) {
+        const int lane = threadIdx.x & 63, i = min(lane, B - 1);
+        const int from = clip(cu[i]), to = clip(cu[i + 1]);
+        const bool below = lane < B && (from >> SHIFT) + PER * i <= at;
+        const int b = max(1, (int)__popcll(__ballot(below))) - 1;
+        first = __builtin_amdgcn_readlane(from, b);
+        n = max(__builtin_amdgcn_readlane(to, b) - first, 0);
+        return b;
+    }
+    const int b = wave_search(B, at, [&](int x) { return (clip(cu[x]) >> SHIFT) + PER * x; });
+    clipped_rows(cu, b, T, first, n);
+    return b;
+}
+
 hipError_t launch_kv8_append(const void *k, const void *v, const KvView &kv, int d_h, const int32_t *cu, int B, int T,
                              hipStream_t st);
 hipError_t launch_kv8_gather(const KvView &kv, int d_h, const int32_t *cu, int B, int T, void *k, void *v, hipStream_t st);

@@ -59,8 +59,7 @@ __device__ inline bool find_slot(const KvView &kv, const int32_t *cu, int B, int
 {
     int b, n, i = 0;
     if (cu) {
-        b = wave_search(B, at, [&](int x) { return (min(max(cu[x], 0), T) >> 4) + 2 * x; });
-        clipped_rows(cu, b, T, s.first_row, n);
+        b = slot_entry<4, 2>(cu, B, T, at, s.first_row, n);
         i = at - (s.first_row >> 4) - 2 * b;
     } else {
         b = at;
@@ -177,9 +176,8 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(GatherParams p)
 {
     constexpr int LPU = D < 64 ? D : 64, PPL = D / LPU, UNITS = 256 / LPU;
     const KvView &kv = p.kv;
-    const int b = wave_search(p.B, blockIdx.x, [&](int x) { return (min(max(p.cu[x], 0), p.T) >> 4) + 2 * x; });
     int row, n;
-    clipped_rows(p.cu, b, p.T, row, n);
+    const int b = slot_entry<4, 2>(p.cu, p.B, p.T, blockIdx.x, row, n);
     const int i = (int)blockIdx.x - (row >> 4) - 2 * b;
     const int seq = kv.seq(b);
     if (n == 0 || i < 0 || seq < 0) return;
