@@ -123,12 +123,35 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     const int half = l >> 5, col = l & 31;
     const int br = w >> 2, group = (w & 3) % S::kGroups, split = (w & 3) / S::kGroups;
 
-    // ---- which rows: the slots of sequence b begin at cu_q[b] / kRows + b; the last ones first (they see the most keys)
-    const int slot = p.slots - 1 - (int)(blockIdx.x / H);
-    int q0, nq, k0, nk;
-    const int b = slot_entry<S::kRows == 128 ? 7 : S::kRows == 64 ? 6 : 5, 1>(a.cu_q, a.B, a.Tq, slot, q0, nq);
-    clipped_rows(a.cu_k, b, a.Tk, k0, nk);
-    const int first = (slot - q0 / S::kRows - b) * S::kRows;
+    // ---- which rows.  Workgroups that see the most keys come first: of up to 64 sequences those with the most keys,
+    // of a sequence the last rows.
+    const int slot = blockIdx.x / H;
+    int b, q0, nq, k0, nk, first;
+    if (a.B <= 64) {
+        int fq, n, fk, m;
+        clipped_rows(a.cu_q, min(l, a.B - 1), a.Tq, fq, n);
+        clipped_rows(a.cu_k, min(l, a.B - 1), a.Tk, fk, m);
+        const int mine = l < a.B ? (n + S::kRows - 1) / S::kRows : 0;
+        int before = 0;                             // tiles of the sequences that come before the lane's
+        for (int j = 0; j < a.B; ++j) {
+            const int mj = __builtin_amdgcn_readlane(m, j);
+            before += mj > m || (mj == m && j < l) ? __builtin_amdgcn_readlane(mine, j) : 0;
+        }
+        const unsigned long long at = __ballot(slot >= before && slot < before + mine);
+        if (!at) return;
+        b = __builtin_ctzll(at);
+        q0 = __builtin_amdgcn_readlane(fq, b);
+        nq = __builtin_amdgcn_readlane(n, b);
+        k0 = __builtin_amdgcn_readlane(fk, b);
+        nk = __builtin_amdgcn_readlane(m, b);
+        first = (__builtin_amdgcn_readlane(before + mine, b) - 1 - slot) * S::kRows;
+    } else {
+        // (the slots of sequence b begin at cu_q[b] / kRows + b)
+        constexpr int SHIFT = S::kRows == 128 ? 7 : S::kRows == 64 ? 6 : 5;
+        b = slot_entry<SHIFT, 1>(a.cu_q, a.B, a.Tq, p.slots - 1 - slot, q0, nq);
+        clipped_rows(a.cu_k, b, a.Tk, k0, nk);
+        first = (p.slots - 1 - slot - (q0 >> SHIFT) - b) * S::kRows;
+    }
     if (first < 0 || first >= nq) return;
     const int row = first + group * 32 + col;       // the lane's query
     const bool real = row < nq;
