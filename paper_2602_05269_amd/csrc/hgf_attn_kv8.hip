@@ -318,7 +318,7 @@ __global__ __launch_bounds__(512) void kv8_merge_kernel(Kv8AttnParams p)
 
 // Parts of every sequence: enough workgroups to fill the chip several times over, none of fewer than 256 positions of
 // the table's capacity.  Tables of up to 1024 positions are one part, taken by workgroups of eight wavefronts: two
-// tiles a wavefront at most cost less than the merge's launch (24 sequences of up to 512, 8 heads of 32: 7.9 us, in three
+// tiles a wavefront at most cost less than the merge's launch (24 sequences of up to 512, 8 heads of 32: 7.2 us, in three
 // parts of four wavefronts 8.6 and 3.7).
 constexpr int kOnePart = 1024;
 int parts_of(int B, long long capacity, int n_heads)

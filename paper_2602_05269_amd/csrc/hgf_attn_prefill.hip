@@ -18,12 +18,10 @@
 // given, both only in tiles that need them; tiles whose document numbers lie outside those of the rows are not
 // read.  What a row does not see has weight 0; values of V that are no finite numbers are taken out of the tile and
 // added to the rows that see them (0 * inf would reach the others).
-// What a tile of 64 keys costs a compute unit (64 columns, 32 heads, 4096 rows without causality: 1.4 us): 1024 clocks of
-// matrix instructions, about as many of vector instructions per pair of wavefronts (exponentials 8 clocks, maxima, conversions and
-// dot products 4, the rest 2.5), LDS reads and the barrier.  They add up rather than overlap, with two wavefronts on a SIMD
-// as with four, with the branches' phases set against each other and with the next tile's scores computed during
-// the exponentials (measured: 1.4 to 1.5 all of them), and the clock falls to 1.9 GHz under this load (1.5 under random matrix products
-// alone): 770 TFLOP/s, 860 with 128 columns, against 1350 of a plain matrix product of 8192.
+// Bound by the chip's power limit: with two wavefronts to a SIMD a pass of 4096 rows, 32 heads of 64 columns took 404 000 clocks
+// at 1.97 GHz, with four 340 000 at 1.74 GHz, and taking out any part (staging, matrix instructions, exponentials) saves
+// about that part's time alone.  184 us, 745 TFLOP/s (770 without causality, 865 with 128 columns), against 1350 of a
+// plain matrix product of 8192.
 #include "hgf_kv8.h"
 
 #include <limits.h>
