@@ -77,11 +77,11 @@ def test_append_of_more_tokens_than_positions_and_to_missing_pages():
     assert np.array_equal(vv.cpu().numpy().astype(np.float64), t.pools[0][1].read(t.ref.table[0], range(40)))
 
 
-def test_append_of_many_rows():
-    """More batch rows than one step of the search over offsets takes, most of them empty."""
+@pytest.mark.parametrize("B", [64, 65, 300, 4200])
+def test_append_of_many_rows(B):
+    """More batch rows than one, two steps of the search over offsets take, most of them empty."""
     rng = np.random.default_rng(3)
-    B = 300
-    t = Both(400, 16, B, 3, 1, 16)
+    t = Both(3 * B, 16, B, 3, 1, 16)
     n = [int(x) for x in rng.integers(0, 4, B) * rng.integers(0, 12, B)]
     seqs = [int(s) for s in rng.permutation(B)]
     t.grow(seqs, n)

@@ -75,10 +75,11 @@ def test_documents():
     _check(q, k, v, cu, doc_q=[9] * (n + 40), doc_k=rising)
 
 
+@pytest.mark.parametrize("H", [2, 150])                   # workgroups of few rows, and of 128
 @pytest.mark.parametrize("d", [16, 64, 128])
-def test_infinities_and_what_is_not_a_number(d):
+def test_infinities_and_what_is_not_a_number(d, H):
     """They reach the rows that see them, and no other."""
-    H, n = 2, 200
+    n = 200
     q, k, v, cu, _, _ = _inputs(6 + d, H, d, [n])
     docs = [0] * 180 + [-1] * 20
     clean = hb.hgf_diff_attention_prefill(dev(q), dev(k), dev(v), ints(cu), 0.8, doc_q=ints(docs), doc_k=ints(docs))
@@ -127,6 +128,87 @@ def test_many_sequences():
     lens = [int(x) for x in rng.integers(0, 6, 500)]
     q, k, v, cu, _, _ = _inputs(10, 1, 16, lens)
     _check(q, k, v, cu)
+
+
+@pytest.mark.parametrize("H,d", [(1, 16), (6, 64), (5, 128)])
+def test_more_sequences_than_lanes(H, d):
+    """70 ragged sequences, in workgroups of 32 (64) and of 128 rows, with and without documents and earlier keys."""
+    rng = np.random.default_rng(H)
+    lq = [int(x) for x in rng.integers(0, 60, 70)]
+    lq[3] = 150
+    lk = [n + int(x) for n, x in zip(lq, rng.integers(0, 30, 70))]
+    q, k, v, cu_q, cu_k, _ = _inputs(13 + d, H, d, lq, lk)
+    docs = [list(rng.integers(-1, 3, n)) for n in lk]
+    doc_k = np.concatenate(docs)
+    doc_q = np.concatenate([x[len(x) - n:] for x, n in zip(docs, lq)])
+    if H == 1:
+        _check(q, k, v, cu_q, cu_k=cu_k)
+    _check(q, k, v, cu_q, cu_k=cu_k, doc_q=doc_q, doc_k=doc_k, prefix=[9] * 70)
+
+
+@pytest.mark.parametrize("H,d,n", [(1, 16, 8500), (8, 64, 4500)])
+def test_documents_over_more_tiles_than_one_window(H, d, n):
+    """Documents far apart: windows of 64 tiles of which all, some or no tile matters; rows against the oracle one by one."""
+    q, k, v, cu, _, rng = _inputs(14 + d, H, d, [n])
+    far = np.full(n, 7)
+    far[:50], far[n - 300:n - 20] = 3, 3                                  # one document at both ends
+    rising = np.sort(rng.integers(0, 12, n))
+    for docs in (far, rising):
+        out = hb.hgf_diff_attention_prefill(dev(q), dev(k), dev(v), ints(cu), 0.8, doc_q=ints(docs), doc_k=ints(docs)).cpu().numpy()
+        for i in [0, 49, 50, n - 301, n - 300, n - 21, n - 20, n - 1] + [int(x) for x in rng.integers(0, n, 6)]:
+            seen = ((np.arange(n) <= i) & (docs == docs[i]))[None, :]
+            ref = ko.attend(q[i:i + 1], k, v, 0.8, seen, np.abs(i - np.arange(n))[None, :])
+            close(out[i:i + 1], ref, float(np.abs(v).max()), 0.8, True, f"row {i}")
+
+
+def test_a_prefix_means_nothing_without_causality_and_is_clipped_with_it():
+    q, k, v, cu, _, _ = _inputs(15, 2, 32, [90, 40])
+    run = lambda **kw: hb.hgf_diff_attention_prefill(dev(q), dev(k), dev(v), ints(cu), 0.8, **kw)
+    assert torch.equal(run(causal=False), run(causal=False, prefix=ints([5, 1000])))
+    assert torch.equal(run(), run(prefix=ints([-3, -2147483648])))
+    assert torch.equal(run(prefix=ints([2147483647, 40])), run(prefix=ints([90, 40])))
+
+
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("kind", ["plain", "cap", "bias", "documents", "earlier keys"])
+def test_workgroups_of_128_rows(d, kind):
+    """So many heads that short sequences fill the chip: every kind of score and mask there, some heads against the oracle."""
+    H, lq = 110, [150, 33, 1, 200]
+    lk = [n + 70 for n in lq] if kind == "earlier keys" else lq
+    q, k, v, cu_q, cu_k, rng = _inputs(18 + d, H, d, lq, lk)
+    slopes = (2.0 ** -rng.uniform(0, 8, 2 * H)).astype(np.float32)
+    docs = np.sort(rng.integers(-1, 4, sum(lk)))
+    kw = {"plain": {}, "cap": dict(softcap=20.0, prefix=[100, 5, 1, 0]), "bias": dict(slopes=slopes, causal=False),
+          "documents": dict(doc_q=docs, doc_k=docs, softcap=600.0, slopes=slopes), "earlier keys": dict(cu_k=cu_k, prefix=[90, 90, 9, 260])}[kind]
+    opt = {n: (ints(x) if n in ("prefix", "doc_q", "doc_k", "cu_k") else dev(x) if n == "slopes" else x) for n, x in kw.items()}
+    out = hb.hgf_diff_attention_prefill(dev(q), dev(k), dev(v), ints(cu_q), 0.8, **opt).cpu().numpy()
+    for h in (0, 57, 109):
+        two = [h, H + h]
+        ref_kw = dict(kw, slopes=slopes[two]) if "slopes" in kw else kw
+        ref = ko.prefill(q[:, two], k[:, two], v[:, [h]], cu_q, 0.8, **ref_kw)
+        close(out[:, [h]], ref, float(np.abs(v).max()), 0.8, True, f"{kind}, head {h}")
+
+
+def test_many_heads():
+    """Rows of a key that are a quarter of a MiB long."""
+    q, k, v, cu, _, _ = _inputs(16, 512, 128, [70])
+    out = hb.hgf_diff_attention_prefill(dev(q), dev(k), dev(v), ints(cu), 0.8).cpu().numpy()
+    for h in (0, 311, 511):
+        ref = ko.prefill(q[:, [h, 512 + h]], k[:, [h, 512 + h]], v[:, [h]], cu, 0.8)
+        close(out[:, [h]], ref, float(np.abs(v).max()), 0.8, True, f"head {h}")
+
+
+def test_two_calls_at_once():
+    q, k, v, cu, _, _ = _inputs(17, 4, 64, [700, 300])
+    a, b = (tuple(dev(t) for t in (q, k, v)) for _ in range(2))
+    a[0].mul_(0.5)
+    want = [hb.hgf_diff_attention_prefill(*x, ints(cu), 0.8) for x in (a, b)]
+    cu_d, streams = ints(cu), [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[hb.hgf_diff_attention_prefill(*x, cu_d, 0.8, stream=s) for s, x in zip(streams, (a, b))] for _ in range(5)]
+    torch.cuda.synchronize()
+    for pair in got:
+        assert torch.equal(pair[0], want[0]) and torch.equal(pair[1], want[1])
 
 
 @pytest.mark.parametrize("H,d,n", [(8, 32, 500), (4, 64, 1500), (2, 128, 1100)])
