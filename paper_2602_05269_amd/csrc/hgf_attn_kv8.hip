@@ -316,15 +316,19 @@ __global__ __launch_bounds__(512) void kv8_merge_kernel(Kv8AttnParams p)
     }
 }
 
-// Parts of every sequence: enough workgroups to fill the chip several times over, none of fewer than 256 positions of
-// the table's capacity.  Tables of up to 1024 positions are one part, taken by workgroups of eight wavefronts: two
+// Parts of every sequence: about as many workgroups as the chip holds at a time (1024 of 64 columns), none of fewer than 256
+// positions of the table's capacity.  More of them start and merge for longer than they level out, fewer leave ragged
+// sequences' ends alone.  (us, for 768 / 1024 / 1536 / 2048 workgroups, caches from memory: 8 ragged ones of up to 4096, 32 heads of 64
+// 31.2 / 29.2 / 32.0 / 33.1, full 45.6 / 44.2 / 48.5 / 45.5; 64 ragged of up to 1200, 16 heads of 64 33.3 / 32.9 / 40.0 / 39.9; 16 ragged of
+// up to 8192, 16 heads of 128 104.8 / 97.6 / 99.9 / 98.9; 2 of 16384, 32 heads of 16 20.7 / 19.3 / 19.8 / 21.3.)
+// Tables of up to 1024 positions are one part, taken by workgroups of eight wavefronts: two
 // tiles a wavefront at most cost less than the merge's launch (24 sequences of up to 512, 8 heads of 32: 7.2 us, in three
 // parts of four wavefronts 8.6 and 3.7).
 constexpr int kOnePart = 1024;
 int parts_of(int B, long long capacity, int n_heads)
 {
     if (capacity <= kOnePart) return 1;
-    const long long most = (capacity + 255) / 256, want = (2048 + (long long)B * n_heads - 1) / ((long long)B * n_heads);
+    const long long most = (capacity + 255) / 256, want = (1024 + (long long)B * n_heads - 1) / ((long long)B * n_heads);
     return (int)(want < 1 ? 1 : want < most ? want : most);
 }
 
