@@ -225,11 +225,12 @@ hgf_status hgf_diff_attention_decode(const void *q_f16, const void *k_cache_f16,
  *   q_f16        fp16 [Tq, 2 n_heads, d_h]    k_f16 fp16 [Tk, 2 n_heads, d_h]    v_f16 fp16 [Tk, n_heads, d_h]
  *   cu_q, cu_k   int32 [B + 1] (device), rising, from 0 .. Tq and 0 .. Tk; cu_k NULL: cu_q (then Tk must be Tq).
  *                Offsets beyond are clipped to the tensor, a sequence whose offsets fall has no rows
+ *                (and where offsets fall, rows of other sequences may be left out)
  *   prefix       int32 [B] (device) or NULL: so many keys of the sequence are seen from every row
  *   doc_q, doc_k int32 [Tq], int32 [Tk] (device), both or none: document numbers in any order; negative: padding, which sees
  *                nothing and is not seen
  *   softcap      0 (none) or 1e-20 .. 1e20
- *   slopes       fp32 [2 n_heads] (device) or NULL: a distance bias per head of q
+ *   slopes       fp32 [2 n_heads] (device) or NULL: a distance bias per head of q, of magnitudes up to 1e30
  *   out_f16      fp16 [Tq, n_heads, d_h]; rows in front of cu_q[0] and behind cu_q[B] are left as they are
  * d_h 16, 32, 64 or 128; n_heads <= 1024; Tq, Tk < 2^24.  fp32 scores and sums; the softmax weights are
  * rounded to fp16 for the matrix cores.  What a row does not see does not change it, infinities and what is not a

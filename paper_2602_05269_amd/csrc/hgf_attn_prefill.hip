@@ -9,8 +9,8 @@
 // wavefront), and the 8 weights of a step that a lane holds after S^T are the ones it has to supply for O^T if V's
 // keys are taken in the order in which the accumulator's rows lie (4 h .. 4 h + 3 and 8 + 4 h .. for half h): P never
 // moves.  V is transposed by the LDS reads that fetch it.
-// Few rows would leave most of the chip idle: then (SPLIT) a workgroup holds 32 rows, takes 128 keys at a time, and its
-// wavefronts share the keys of a tile; they are merged at the end.
+// Few rows would leave most of the chip idle: then (SPLIT) a workgroup holds 32 rows and takes 128 keys at a time (128 columns: 64
+// and 64), and its wavefronts share the keys of a tile; they are merged at the end.
 // Weights are relative to the running maximum in base 2 and carried 2^7 larger, so that fp16 holds them down to
 // 2^-31; a row's maximum is only raised when a tile exceeds it by 2^8 (which the factor leaves room for), which spares
 // most rescalings.  fp32: scores, weights before rounding, sums, outputs.  The sum adds up the rounded weights.
@@ -44,7 +44,7 @@ constexpr float kCoarseCap = 512.0f;
 struct PrefillParams {
     PrefillArgs a;
     float scale;
-    int slots;
+    int slots, layer;
 };
 
 // Sizes of one variant.
@@ -77,7 +77,6 @@ __device__ inline int opaque(int v)
     asm volatile("" : "+v"(v));
     return v;
 }
-// The larger of a lane's value and of the lane 32 further on or back.
 // 64 x 16 bytes from memory straight into LDS, in flight until a wait on vmcnt.  (In assembly because with the builtin the compiler
 // waits for everything in flight before the transposing LDS reads, whichever buffer they read.  Nothing comes back in
 // registers, and the kernel's own waits are the only ones that are needed.)
@@ -98,6 +97,7 @@ __device__ inline v4u rsrc_words(const void *base, unsigned bytes)
     const uint64_t a = reinterpret_cast<uint64_t>(base);
     return v4u{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, bytes, 0x00020000u};
 }
+// The larger of a lane's value and of the lane 32 further on or back.
 __device__ inline float halves_max(float v)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
 
     // ---- which rows.  Workgroups that see the most keys come first: of up to 64 sequences those with the most keys,
     // of a sequence the last rows.
-    const int slot = blockIdx.x / H;
+    const int slot = blockIdx.y * p.layer + blockIdx.x / H;
     int b, q0, nq, k0, nk, first;
     if (a.B <= 64) {
         int fq, n, fk, m;
@@ -145,6 +145,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         first = (__builtin_amdgcn_readlane(before + mine, b) - 1 - slot) * S::kRows;
     } else {
         // (the slots of sequence b begin at cu_q[b] / kRows + b)
+        if (slot >= p.slots) return;
         constexpr int SHIFT = S::kRows == 128 ? 7 : S::kRows == 64 ? 6 : 5;
         b = slot_entry<SHIFT, 1>(a.cu_q, a.B, a.Tq, p.slots - 1 - slot, q0, nq);
         clipped_rows(a.cu_k, b, a.Tk, k0, nk);
@@ -596,8 +597,13 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
         static OncePerDevice once;
         e = allow_lds(once, (const void *)(prefill_attn_kernel<D, MOD, SPLIT>), S::kLds);
         p.slots = a.Tq / S::kRows + a.B;
+        // (one dimension of a grid, unless many heads of many sequences are more threads than it may have: heads, slots and layers
+        // as three dimensions took 187 us where one takes 181)
+        const int most = (int)(((1u << 31) / kThreads) / a.n_heads);
+        p.layer = p.slots < most ? p.slots : most;
+        const dim3 grid((unsigned)(p.layer * a.n_heads), (p.slots + p.layer - 1) / p.layer);
         if (e == hipSuccess)
-            hipLaunchKernelGGL((prefill_attn_kernel<D, MOD, SPLIT>), dim3((unsigned)p.slots * a.n_heads), dim3(kThreads), S::kLds, st, p);
+            hipLaunchKernelGGL((prefill_attn_kernel<D, MOD, SPLIT>), grid, dim3(kThreads), S::kLds, st, p);
     };
     auto variant = [&](auto d, auto m) {
         if (few) go(d, m, std::integral_constant<int, decltype(d)::value == 128 ? 2 : 4>{});

@@ -198,6 +198,20 @@ def test_many_heads():
         close(out[:, [h]], ref, float(np.abs(v).max()), 0.8, True, f"head {h}")
 
 
+def test_many_heads_of_many_sequences():
+    """More threads than a grid may have in one dimension: 2^13 + 300 sequences of one token, 1024 heads.  A row sees one key, so it
+    is (1 - lambda) / 2 of its value: the weight cancels in a quotient, four roundings in fp32 and one to fp16."""
+    B, H, d = 8492, 1024, 16
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    q, k = (torch.randn((B, 2 * H, d), generator=gen, device="cuda", dtype=torch.float16) for _ in range(2))
+    v = torch.randn((B, H, d), generator=gen, device="cuda", dtype=torch.float16)
+    out = hb.hgf_diff_attention_prefill(q, k, v, torch.arange(B + 1, dtype=torch.int32, device="cuda"), 0.25)
+    ref = v.double() * 0.375
+    # each branch is within 3 * 2^-24 of 0.5 and 0.125 times the value; fp16: half a step, or half of 2^-24 below its normal numbers
+    bound = ref.abs() * 2.0 ** -11 + v.double().abs() * (0.625 * 4 * 2.0 ** -24) + 2.0 ** -25
+    assert bool(((out.double() - ref).abs() <= bound * 1.001).all())
+
+
 def test_two_calls_at_once():
     q, k, v, cu, _, _ = _inputs(17, 4, 64, [700, 300])
     a, b = (tuple(dev(t) for t in (q, k, v)) for _ in range(2))
