@@ -58,6 +58,19 @@ def test_one_long_sequence_in_many_parts():
         _check(t, half(rng, 1, 2, 16), [0])
 
 
+@pytest.mark.parametrize("d,lens", [(16, [1030, 33]), (32, [0, 700]), (64, [200, 1]), (128, [90, 0])])
+def test_many_heads_over_a_long_table(d, lens):
+    """So many heads that a sequence is one part although its table has room for more than 1024 positions."""
+    rng = np.random.default_rng(18 + d)
+    H = 512
+    t = Both(sum(n // 16 + 1 for n in lens), 16, 2, 65, H, d)
+    assert hb.hgf_diff_attention_kv8_workspace_bytes(2, t.pages, H, d) == 0
+    t.place(lens, rng)
+    t.fill(rng)
+    _check(t, half(rng, 2, 2 * H, d), [0, 1])
+    _check(t, half(rng, 2, 2 * H, d), [1, 0], softcap=30.0, slopes=(2.0 ** -rng.uniform(0, 8, 2 * H)).astype(np.float32))
+
+
 def test_blocks_of_very_different_scales_and_peaked_scores():
     """V's scales and the softmax spread over many powers of two inside one tile of positions."""
     rng = np.random.default_rng(12)
