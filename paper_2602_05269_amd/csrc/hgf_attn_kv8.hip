@@ -68,27 +68,20 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
 {
     constexpr int LD = D / 16;                      // 16-byte loads per lane of one head of K (or V) for 64 positions
     constexpr int QC = D == 128 ? 2 : 1;            // chunks of 16 columns whose digits a lane holds
-    __shared__ __align__(16) unsigned char dig[WAVES][8][kTile];
+    __shared__ __align__(16) unsigned char dig[WAVES][8][kTile], q_dig[2][4][D];
     __shared__ float o_s[WAVES][2][D], m_s[WAVES][2], l_s[WAVES][2];
     const KvView &kv = p.kv;
     const int H = kv.n_heads, h = blockIdx.x, part = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, l = tid & 63, g = l >> 4, r = l & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (q is requested before anything is known of the sequence: fewer trips to memory one after the other)
-    v8h q_raw[2][QC][2];
     _Float16 q_own[2][LD];
 #pragma unroll
-    for (int br = 0; br < 2; ++br) {
-        const _Float16 *qr = p.q + ((size_t)b * 2 * H + br * H + h) * D;
+    for (int br = 0; br < 2; ++br)
 #pragma unroll
-        for (int c = 0; c < LD; ++c) q_own[br][c] = qr[c * 16 + r];
-#pragma unroll
-        for (int i = 0; i < QC; ++i) {
-            const v8h *src = reinterpret_cast<const v8h *>(qr + (i * 4 + g % LD) * 16);     // (D < 64: the k-groups repeat the chunks)
-            q_raw[br][i][0] = src[0];
-            q_raw[br][i][1] = src[1];
-        }
-    }
+        for (int c = 0; c < LD; ++c) q_own[br][c] = p.q[((size_t)b * 2 * H + br * H + h) * D + c * 16 + r];
+    const int my_br = tid / D & 1;                  // the thread's column of q, for its digits
+    const _Float16 q_mine = p.q[((size_t)b * 2 * H + my_br * H + h) * D + tid % D];
     const int seq = kv.seq(b);
     const int len = seq >= 0 ? kv.len(seq) : 0;
     const int tiles = (len + kTile - 1) / kTile, each = (tiles + p.parts - 1) / p.parts;
@@ -99,9 +92,10 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
         return;
     }
 
-    // ---- q as digits: lane l holds digit r mod 4 of the columns that its k-group g takes in each load
+    // ---- q as digits: a thread takes a column apart, lane l holds digit r mod 4 of the columns that its k-group g takes in each
+    // load (D < 64: the k-groups repeat the columns)
     v4i qd[2][QC];
-    float q_scale[2];
+    float q_scale[2], f[2];
     bool odd = false;
 #pragma unroll
     for (int br = 0; br < 2; ++br) {
@@ -113,27 +107,22 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
             amax = x <= 65504.0f ? fmaxf(amax, x) : amax;
         }
         amax = wave_max(amax);
-        const float f = fixed_point(amax);
-        q_scale[br] = amax > 0.0f ? reciprocal_of_power(f) * p.scale : 0.0f;
-#pragma unroll
-        for (int i = 0; i < QC; ++i) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const v8h x = q_raw[br][i][half];
-                uint32_t word[2] = {0, 0};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    int d[3];
-                    const float v = (float)x[e];
-                    digits_of((int)rintf(fabsf(v) <= 65504.0f ? v * f : 0.0f), d);
-                    const int mine = (r & 3) == 0 ? d[0] : (r & 3) == 1 ? d[1] : (r & 3) == 2 ? d[2] : 0;
-                    word[e >> 2] |= (uint32_t)(mine & 0xff) << (8 * (e & 3));
-                }
-                qd[br][i][2 * half] = (int)word[0];
-                qd[br][i][2 * half + 1] = (int)word[1];
-            }
-        }
+        f[br] = fixed_point(amax);
+        q_scale[br] = amax > 0.0f ? reciprocal_of_power(f[br]) * p.scale : 0.0f;
     }
+    if (tid < 2 * D) {
+        const float x = (float)q_mine;
+        int d[3];
+        digits_of((int)rintf(fabsf(x) <= 65504.0f ? x * (my_br ? f[1] : f[0]) : 0.0f), d);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) q_dig[my_br][i][tid % D] = (unsigned char)d[i];
+        q_dig[my_br][3][tid % D] = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int br = 0; br < 2; ++br)
+#pragma unroll
+        for (int i = 0; i < QC; ++i) qd[br][i] = *reinterpret_cast<const v4i *>(&q_dig[br][r & 3][(i * 4 + g % LD) * 16]);
     odd = __any(odd);
 
     float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, o[LD];
