@@ -92,6 +92,8 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
         return;
     }
 
+    int own_next = kv.page_of(seq, (t0 + w) * 4 + g);           // (a tile ahead: of the lane's own block of 16 positions)
+
     // ---- q as digits: a thread takes a column apart, lane l holds digit r mod 4 of the columns that its k-group g takes in each
     // load (D < 64: the k-groups repeat the columns)
     v4i qd[2][QC];
@@ -138,7 +140,8 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
     for (int tile = t0 + w; tile < t1; tile += WAVES) {
         const int pos = tile * kTile + l;
         const int blk = tile * 4 + g;               // the lane's own block of 16 positions
-        const int own = kv.page_of(seq, blk);
+        const int own = own_next;
+        own_next = kv.page_of(seq, blk + 4 * WAVES);
         const bool valid = pos < len && own >= 0;
         const int page = max(own, 0);               // (where there is none: any address inside the pool)
         // block numbers of the lane's own block in the pools of K (both branches) and V
