@@ -11,7 +11,7 @@
 //     V serves both branches, lane l holds branch (l / 16) mod 2 of columns 16 t + l mod 16.
 // The integer sums are exact, a digit sum stays below 2^21, and what is rounded is q and a weight to 23 bits
 // each, below fp32's own rounding of the products.  Running maximum, sums and the outputs between tiles are fp32.
-// A wavefront takes tiles of 64 positions; a workgroup of four merges its wavefronts in LDS; with more than one part
+// A wavefront takes tiles of 64 positions; a workgroup of four or eight merges its wavefronts in LDS; with more than one part
 // of a sequence, a second launch merges the parts.  The parts of a sequence follow from its length on the device, their number
 // from the batch and the table's capacity.
 #include "hgf_kv8.h"
@@ -34,6 +34,9 @@ struct Kv8AttnParams {
     int parts;
     float lambda, softcap, scale;
 };
+
+// Tiles of each part of a sequence: no fewer than the wavefronts of a workgroup.
+__device__ inline int part_tiles(int tiles, int parts) { return max((tiles + parts - 1) / parts, 4); }
 
 // 2^(21 - exponent of v) for positive v: v times it lies in [2^21, 2^22), so its top digit of base 256 fits int8.
 __device__ inline float fixed_point(float v)
@@ -63,9 +66,11 @@ __device__ inline float soft_cap(float x, float cap, float inv)
     return cap * (fabsf(y) < 0.3f ? series : t);
 }
 
-template <int D, bool MOD, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
+// ONE: one part per sequence, eight wavefronts, and no merge afterwards.
+template <int D, bool MOD, bool ONE>
+__global__ __launch_bounds__(ONE ? 512 : 256) void kv8_attn_kernel(Kv8AttnParams p)
 {
+    constexpr int WAVES = ONE ? 8 : 4;
     constexpr int LD = D / 16;                      // 16-byte loads per lane of one head of K (or V) for 64 positions
     constexpr int QC = D == 128 ? 2 : 1;            // chunks of 16 columns whose digits a lane holds
     __shared__ __align__(16) unsigned char dig[WAVES][8][kTile], q_dig[2][4][D];
@@ -84,11 +89,11 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
     const _Float16 q_mine = p.q[((size_t)b * 2 * H + my_br * H + h) * D + tid % D];
     const int seq = kv.seq(b);
     const int len = seq >= 0 ? kv.len(seq) : 0;
-    const int tiles = (len + kTile - 1) / kTile, each = (tiles + p.parts - 1) / p.parts;
+    const int tiles = (len + kTile - 1) / kTile, each = part_tiles(tiles, p.parts);
     const int t0 = part * each, t1 = min(t0 + each, tiles);
     _Float16 *out = p.out + ((size_t)b * H + h) * D;
     if (t0 >= t1) {                                 // (the merge reads no such part)
-        if (p.parts == 1 && tid < D) out[tid] = (_Float16)0.0f;
+        if (ONE && tid < D) out[tid] = (_Float16)0.0f;
         return;
     }
 
@@ -237,7 +242,7 @@ __global__ __launch_bounds__(64 * WAVES) void kv8_attn_kernel(Kv8AttnParams p)
         }
         if (odd) acc = __builtin_nanf("");
     }
-    if (p.parts == 1) {
+    if (ONE) {
         if (br < 2) o_s[0][br][d] = total > 0.0f ? acc / total : odd ? acc : 0.0f;      // (its own element)
         __syncthreads();
         if (br == 0) out[d] = (_Float16)((o_s[0][0][d] - p.lambda * o_s[0][1][d]) * 0.5f);
@@ -260,7 +265,7 @@ __global__ __launch_bounds__(512) void kv8_merge_kernel(Kv8AttnParams p)
     __shared__ float red[GROUPS][2][D], top_s[2], sum_s[2];
     const int H = p.kv.n_heads, h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int seq = p.kv.seq(b);
-    const int tiles = seq >= 0 ? (p.kv.len(seq) + kTile - 1) / kTile : 0, each = (tiles + p.parts - 1) / p.parts;
+    const int tiles = seq >= 0 ? (p.kv.len(seq) + kTile - 1) / kTile : 0, each = part_tiles(tiles, p.parts);
     const int used = tiles > 0 ? (tiles + each - 1) / each : 0;
     const float *part = p.part + ((size_t)b * H + h) * p.parts * 2 * (D + 2);
     if (tid < 128) {
@@ -308,20 +313,26 @@ __global__ __launch_bounds__(512) void kv8_merge_kernel(Kv8AttnParams p)
     }
 }
 
-// Parts of every sequence: about as many workgroups as the chip holds at a time (1024 of 64 columns), none of fewer than 256
-// positions of the table's capacity.  More of them start and merge for longer than they level out, fewer leave ragged
-// sequences' ends alone.  (us, for 768 / 1024 / 1536 / 2048 workgroups, caches from memory: 8 ragged ones of up to 4096, 32 heads of 64
-// 31.2 / 29.2 / 32.0 / 33.1, full 45.6 / 44.2 / 48.5 / 45.5; 64 ragged of up to 1200, 16 heads of 64 33.3 / 32.9 / 40.0 / 39.9; 16 ragged of
-// up to 8192, 16 heads of 128 104.8 / 97.6 / 99.9 / 98.9; 2 of 16384, 32 heads of 16 20.7 / 19.3 / 19.8 / 21.3.)
-// Tables of up to 1024 positions are one part, taken by workgroups of eight wavefronts: two
-// tiles a wavefront at most cost less than the merge's launch (24 sequences of up to 512, 8 heads of 32: 7.2 us, in three
-// parts of four wavefronts 8.6 and 3.7).
-constexpr int kOnePart = 1024;
+// Parts of every sequence.  One, taken by workgroups of eight wavefronts, in tables of up to 1024 positions and, up to 8192, where
+// there are so many sequences and heads that their lengths level each other out, 12 positions of capacity or fewer to
+// each: no second launch.  (us, one part of eight wavefronts / several of four, caches from memory: 8 sequences of up to 1024, 8 heads of
+// 32 6.1 / 7.4, of up to 2048 8.8 / 7.7; 20 of up to 2048, 8 of 32 9.5 / 10.4; 16 of up to 3000, 16 of 32 13.5 / 14.4; 16 of up to 4096,
+// 16 of 128 52.3 / 50.2; 32 of up to 4096, 16 of 64 48.4 / 53.1; 16 of up to 8192, 16 of 128 93.5 / 88.4; 32 of up to 8192, 32 of 32
+// 85.2 / 90.8.)
+// Else the larger of two numbers, and none of fewer than 256 positions:
+// - about as many workgroups as the chip holds at a time (1024 of 64 columns).  More of them start and merge for longer than they
+//   level out, fewer leave ragged sequences' ends alone.  (us, for 768 / 1024 / 1536 workgroups: 8 ragged of up to 4096, 32 heads of 64
+//   28.1 / 26.5 / 27.4, full 42.5 / 41.8 / 43.7; 16 ragged of up to 8192, 16 of 128 104.2 / 94.4 / 96.1.)
+// - parts of up to 4096 positions, within 16384 workgroups, for the long sequence among short ones.  (us, without / with, 64 sequences,
+//   16 heads of 64, one of 65536 positions and the others below 1200 314 / 78; ragged ones of up to 16384 383 / 351; where none
+//   is long after all, 37 / 43.)
 int parts_of(int B, long long capacity, int n_heads)
 {
-    if (capacity <= kOnePart) return 1;
-    const long long most = (capacity + 255) / 256, want = (1024 + (long long)B * n_heads - 1) / ((long long)B * n_heads);
-    return (int)(want < 1 ? 1 : want < most ? want : most);
+    const long long rows = (long long)B * n_heads;
+    if (capacity <= 1024 || (capacity <= 8192 && capacity <= 12 * rows)) return 1;
+    const long long fill = (1024 + rows - 1) / rows, room = 16384 / rows, cut = (capacity + 4095) / 4096, most = (capacity + 255) / 256;
+    const long long parts = fill > room || fill > cut ? fill : room < cut ? room : cut;
+    return (int)(parts < most ? parts : most);
 }
 
 }  // namespace
@@ -346,14 +357,14 @@ hipError_t launch_diff_attn_kv8(const void *q, const KvView &kv, int B, int d_h,
     p.softcap = softcap;
     p.scale = 1.0f / sqrtf((float)d_h);
     const dim3 grid(kv.n_heads, p.parts, B);
-    const bool mod = softcap > 0.0f || slopes, one = ((long long)kv.max_pages << kv.page_log2) <= kOnePart;
+    const bool mod = softcap > 0.0f || slopes, one = p.parts == 1;
     auto go = [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (one && mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true, 8>), grid, dim3(512), 0, st, p);
-        else if (one) hipLaunchKernelGGL((kv8_attn_kernel<D, false, 8>), grid, dim3(512), 0, st, p);
-        else if (mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true, 4>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((kv8_attn_kernel<D, false, 4>), grid, dim3(256), 0, st, p);
-        if (p.parts > 1) hipLaunchKernelGGL(kv8_merge_kernel<D>, dim3(kv.n_heads, B), dim3(512), 0, st, p);
+        if (one && mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true, true>), grid, dim3(512), 0, st, p);
+        else if (one) hipLaunchKernelGGL((kv8_attn_kernel<D, false, true>), grid, dim3(512), 0, st, p);
+        else if (mod) hipLaunchKernelGGL((kv8_attn_kernel<D, true, false>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((kv8_attn_kernel<D, false, false>), grid, dim3(256), 0, st, p);
+        if (!one) hipLaunchKernelGGL(kv8_merge_kernel<D>, dim3(kv.n_heads, B), dim3(512), 0, st, p);
     };
     switch (d_h) {
         case 16: go(std::integral_constant<int, 16>{}); break;

@@ -71,6 +71,18 @@ def test_many_heads_over_a_long_table(d, lens):
     _check(t, half(rng, 2, 2 * H, d), [1, 0], softcap=30.0, slopes=(2.0 ** -rng.uniform(0, 8, 2 * H)).astype(np.float32))
 
 
+def test_one_long_sequence_among_many_short_ones():
+    """Parts that follow from the table's capacity: short sequences have fewer of them, some exactly one tile or part."""
+    rng = np.random.default_rng(19)
+    H, d, page = 24, 16, 64
+    lens = [11000, 0, 1, 64, 255, 256, 257, 511, 512, 513, 768, 769] + [int(x) for x in rng.integers(0, 200, 48)]
+    t = Both(sum(n // page + 1 for n in lens), page, len(lens), 180, H, d)
+    assert hb.hgf_diff_attention_kv8_workspace_bytes(len(lens), t.pages, H, d) > 0
+    t.place(lens, rng)
+    t.fill(rng)
+    _check(t, half(rng, len(lens), 2 * H, d), list(range(len(lens))))
+
+
 def test_blocks_of_very_different_scales_and_peaked_scores():
     """V's scales and the softmax spread over many powers of two inside one tile of positions."""
     rng = np.random.default_rng(12)
