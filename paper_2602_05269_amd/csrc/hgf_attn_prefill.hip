@@ -154,6 +154,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
     if (first < 0 || first >= nq) return;
     const int row = first + group * 32 + col;       // the lane's query
     const bool real = row < nq;
+    // the queries, operand B of S^T (requested before anything else is looked up)
+    v8h q[KS];
+    {
+        const _Float16 *src = a.q + ((size_t)(q0 + min(row, nq - 1)) * 2 * H + br * H + h) * D + half * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h *>(src + s * 16);
+    }
     const int pos = nk - nq + row;                  // its position among the keys
     int limit = a.causal ? max(pos + 1, a.prefix ? a.prefix[b] : 0) : nk;       // it sees keys below
     limit = min(max(limit, 0), nk);
@@ -201,15 +208,6 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
         whole = min(tiles, __builtin_amdgcn_readfirstlane(all / S::kKeys));
     }
 
-    // ---- the queries, operand B of S^T
-    v8h q[KS];
-    {
-        const _Float16 *src = a.q + ((size_t)(q0 + min(row, nq - 1)) * 2 * H + br * H + h) * D + half * 8;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h *>(src + s * 16);
-    }
-#pragma unroll
-    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));     // (they are waited for here, not in the loop)
     const float cap = a.softcap, cap_in = cap > 0.0f ? p.scale / cap * (2.0f * kLog2e) : 0.0f, cap_out = cap * kLog2e;
     float slope = 0.0f;
     if (MOD && a.slopes) slope = a.slopes[br * H + h] * kLog2e;
@@ -285,6 +283,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             }
         }
     };
+
+    if (!a.doc_k) {                                 // (with documents it is not known yet which tiles)
+        if (tiles > 0) request(0, 0);
+        if (tiles > 1) request(1, 1);
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));     // (they are waited for here, not in the loop)
 
     float m = -INFINITY, sum = 0.0f;
     v16f o[DT];
@@ -487,8 +492,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefill_attn_kernel(PrefillParams
             return rest ? from + (int)__builtin_ctzll(rest) : stop;
         };
         int tile = a.doc_k ? from + (int)__builtin_ctzll(visit) : 0, next = after(tile), buf = 0;
-        request(tile, 0);
-        if (next < stop) request(next, 1);
+        if (a.doc_k) {
+            request(tile, 0);
+            if (next < stop) request(next, 1);
+        }
         settle(tile, 0, next < stop);
         __syncthreads();
         auto step = [&](auto masked) {
