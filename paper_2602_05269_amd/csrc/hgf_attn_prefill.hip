@@ -9,8 +9,8 @@
 // wavefront), and the 8 weights of a step that a lane holds after S^T are the ones it has to supply for O^T if V's
 // keys are taken in the order in which the accumulator's rows lie (4 h .. 4 h + 3 and 8 + 4 h .. for half h): P never
 // moves.  V is transposed by the LDS reads that fetch it.
-// Few rows would leave most of the chip idle: then (SPLIT) a workgroup holds 32 rows and takes 128 keys at a time (128 columns: 64
-// and 64), and its wavefronts share the keys of a tile; they are merged at the end.
+// Few rows would leave most of the chip idle: then (SPLIT) a workgroup holds 64 rows, or 32 and takes 128 keys at a time, and its
+// wavefronts share the keys of a tile; they are merged at the end.
 // Weights are relative to the running maximum in base 2 and carried 2^7 larger, so that fp16 holds them down to
 // 2^-31; a row's maximum is only raised when a tile exceeds it by 2^8 (which the factor leaves room for), which spares
 // most rescalings.  fp32: scores, weights before rounding, sums, outputs.  The sum adds up the rounded weights.
@@ -589,16 +589,22 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
     p.a = a;
     p.scale = 1.0f / sqrtf((float)d_h);
     const bool mod = a.softcap > 0.0f || a.slopes;
-    // Few workgroups of 128 rows: 32 rows each instead (128 columns, for whose tiles of 128 keys LDS has no room three
-    // times: 64).  It is the faster one up to about 256 workgroups of 128 rows, one to a compute unit, and with 64 columns up
-    // to somewhat fewer.  (us, 128 rows / few, causal: 1000 rows of 32 heads of 32 columns 21.8 / 21.0, 2000 of 16 37.7 / 30.5, of 32
-    // 48 / 58; 64 columns, 1000 rows of 16 heads 27.3 / 20.4, of 32 28.6 / 38.7; 128 columns, 2000 of 16 77 / 69, of 32 98 / 132;
-    // 500 rows of 8 heads of 32, 64, 128 columns 12.8 / 8.1, 16.5 / 10.1, 24.6 / 20.1.  Rows behind many earlier keys all see
-    // about as many, which leaves smaller pieces less to level out: 1900 rows and 7600 keys, 16 heads of 128, 177 / 197.)
-    const bool few = (long long)(a.Tq / 128 + a.B) * a.n_heads < (d_h == 64 || a.Tk / 2 > a.Tq ? 200 : 300);
+    // Rows per workgroup.  128 need the fewest reads, but few of them leave compute units idle, and of causal ones, one or two to a
+    // unit, the last rows' decide: then 64 rows each, and 32 where even those are few.  Where all rows see about as many
+    // keys (not causal, or behind many earlier keys) there is nothing to level out, and 128 are the faster ones from 200 workgroups
+    // on.  (us, 128 / 64 / 32 rows: 32 columns, 1000 rows of 16 heads - / 16.0 / 12.4, of 32 21.8 / 18.4 / 20.4, 8000 of 5 134 / 104 / 106,
+    // of 8 151 / 143 / 158, 2000 of 40 53 / 60 / -; 64 columns, 1000 of 16 27.3 / 20.8 / 20.3, of 20 - / 21.7 / 28.1, 2000 of 16 49.5 / 39.0 /
+    // 55.9, of 20 52.5 / 40.8 / 71, of 32 58.9 / 59.7 / 110, 8 times 300 of 16 17.7 / 19.6 / -, 2000 of 16 not causal 50.4 / 54.0 / -, behind
+    // 8000 226 / 223 / -; 128 columns, for whose tiles of 128 keys LDS has no room three times, 2000 of 16 77 / 69, of 32 98 / 132, 1900
+    // rows and 7600 keys, 16 heads, 177 / 197.)
+    const long long wide = (long long)(a.Tq / 128 + a.B) * a.n_heads;       // workgroups of 128 rows
+    const bool alike = !a.causal || a.Tk / 2 > a.Tq;
+    int split;
+    if (d_h == 128) split = wide < (a.Tk / 2 > a.Tq ? 200 : 300) ? 2 : 1;
+    else split = wide < (d_h == 64 ? 130 : alike ? 200 : 256) ? 4 : wide < (alike ? 200 : 400) ? 2 : 1;
     hipError_t e = hipSuccess;
-    auto go = [&](auto d, auto m, auto split) {
-        constexpr int D = decltype(d)::value, SPLIT = decltype(split)::value;
+    auto go = [&](auto d, auto m, auto s) {
+        constexpr int D = decltype(d)::value, SPLIT = decltype(s)::value;
         constexpr bool MOD = decltype(m)::value;
         using S = Shape<D, SPLIT>;
         static OncePerDevice once;
@@ -613,8 +619,9 @@ hipError_t launch_diff_attn_prefill(const PrefillArgs &a, int d_h, hipStream_t s
             hipLaunchKernelGGL((prefill_attn_kernel<D, MOD, SPLIT>), grid, dim3(kThreads), S::kLds, st, p);
     };
     auto variant = [&](auto d, auto m) {
-        if (few) go(d, m, std::integral_constant<int, decltype(d)::value == 128 ? 2 : 4>{});
-        else go(d, m, std::integral_constant<int, 1>{});
+        if (split == 1) go(d, m, std::integral_constant<int, 1>{});
+        else if (split == 2) go(d, m, std::integral_constant<int, 2>{});
+        else if constexpr (decltype(d)::value < 128) go(d, m, std::integral_constant<int, 4>{});
     };
     auto both = [&](auto d) {
         if (mod) variant(d, std::true_type{});

@@ -189,6 +189,27 @@ def test_workgroups_of_128_rows(d, kind):
         close(out[:, [h]], ref, float(np.abs(v).max()), 0.8, True, f"{kind}, head {h}")
 
 
+@pytest.mark.parametrize("d", [16, 32, 64])
+@pytest.mark.parametrize("kind", ["plain", "cap", "documents", "infinities"])
+def test_workgroups_of_64_rows(d, kind):
+    """As many heads as fill the chip by half with 128 rows each; some heads against the oracle, 4 sequences and 70."""
+    H, rng = 50, np.random.default_rng(d)
+    for n, lq in ((H, [150, 33, 1, 200]), (4, [150] + [int(x) for x in rng.integers(0, 60, 69)])):
+        q, k, v, cu, _, rng = _inputs(20 + d, n, d, lq)
+        docs = np.sort(rng.integers(-1, 4, sum(lq)))
+        if kind == "infinities":
+            v[100, :, d - 3], v[170, :, 2] = np.inf, np.nan
+        kw = {"cap": dict(softcap=20.0, prefix=[70] * len(lq)), "documents": dict(doc_q=docs, doc_k=docs)}.get(kind, {})
+        opt = {m: ints(x) if m != "softcap" else x for m, x in kw.items()}
+        out = hb.hgf_diff_attention_prefill(dev(q), dev(k), dev(v), ints(cu), 0.8, **opt).cpu().numpy()
+        for h in {0, n // 2, n - 1}:
+            two = [h, n + h]
+            ref = ko.prefill(q[:, two], k[:, two], v[:, [h]], cu, 0.8, **kw)
+            known, vmax = np.isfinite(ref), float(np.abs(v[np.isfinite(v)]).max())
+            assert np.array_equal(np.isfinite(out[:, [h]]), known), f"{kind}, {len(lq)} sequences, head {h}"
+            close(out[:, [h]][known], ref[known], vmax, 0.8, True, f"{kind}, {len(lq)} sequences, head {h}")
+
+
 def test_many_heads():
     """Rows of a key that are a quarter of a MiB long."""
     q, k, v, cu, _, _ = _inputs(16, 512, 128, [70])
