@@ -20,7 +20,7 @@
 // added to the rows that see them (0 * inf would reach the others).
 // Bound by the chip's power limit: with two wavefronts to a SIMD a pass of 4096 rows, 32 heads of 64 columns took 404 000 clocks
 // at 1.97 GHz, with four 340 000 at 1.74 GHz, and taking out any part (staging, matrix instructions, exponentials) saves
-// about that part's time alone.  184 us, 745 TFLOP/s (770 without causality, 865 with 128 columns), against 1350 of a
+// about that part's time alone.  184 to 195 us by the card, 745 TFLOP/s (770 without causality, 865 with 128 columns), against 1350 of a
 // plain matrix product of 8192.
 #include "hgf_kv8.h"
 
