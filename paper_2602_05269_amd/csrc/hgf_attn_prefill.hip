@@ -79,17 +79,19 @@ __device__ inline int opaque(int v)
 }
 // 64 x 16 bytes from memory straight into LDS, in flight until a wait on vmcnt.  (In assembly because with the builtin the compiler
 // waits for everything in flight before the transposing LDS reads, whichever buffer they read.  Nothing comes back in
-// registers, and the kernel's own waits are the only ones that are needed.)
+// registers, and the kernel's own waits are the only ones that are needed.  Five wait states lie between whatever stands in front and
+// the load: that many the hardware wants after a vector instruction that wrote the descriptor's registers, as one does that
+// fetches them from where they were spilled; the compiler keeps them for its own loads only.)
 __device__ inline void load_to_lds(v4u rsrc, unsigned lds_byte, unsigned lane_off)
 {
     unsigned kept;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(kept) : "s"(lds_byte), "v"(lane_off), "s"(rsrc) : "memory");
 }
 __device__ inline void load4_to_lds(v4u rsrc, unsigned lds_byte, unsigned lane_off)      // 64 x 4 bytes
 {
     unsigned kept;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(kept) : "s"(lds_byte), "v"(lane_off), "s"(rsrc) : "memory");
 }
 __device__ inline v4u rsrc_words(const void *base, unsigned bytes)
