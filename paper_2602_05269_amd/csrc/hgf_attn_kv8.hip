@@ -243,7 +243,7 @@ __global__ __launch_bounds__(ONE ? 512 : 256) void kv8_attn_kernel(Kv8AttnParams
         if (odd) acc = __builtin_nanf("");
     }
     if (ONE) {
-        if (br < 2) o_s[0][br][d] = total > 0.0f ? acc / total : odd ? acc : 0.0f;      // (its own element)
+        if (br < 2) o_s[0][br][d] = total > 0.0f ? acc / total : 0.0f;      // (its own element; nothing seen: 0, whatever q is)
         __syncthreads();
         if (br == 0) out[d] = (_Float16)((o_s[0][0][d] - p.lambda * o_s[0][1][d]) * 0.5f);
     } else if (br < 2) {
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(512) void kv8_merge_kernel(Kv8AttnParams p)
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < GROUPS; ++i) s += red[i][br][tid];
-            o[br] = sum_s[br] > 0.0f ? s / sum_s[br] : s;           // (nothing seen: s is 0, or NaN from q)
+            o[br] = sum_s[br] > 0.0f ? s / sum_s[br] : 0.0f;        // (nothing seen: 0, whatever q is)
         }
         p.out[((size_t)b * H + h) * D + tid] = (_Float16)((o[0] - p.lambda * o[1]) * 0.5f);
     }
