@@ -57,13 +57,12 @@ __device__ inline float join_digits(v4i a)
 {
     return __builtin_fmaf((float)a[0], 65536.0f, __builtin_fmaf((float)a[1], 256.0f, (float)a[2]));
 }
-// cap tanh(x / cap); for small arguments the series, where 1 - 2 / (e + 1) would cancel
+// cap tanh(x / cap)
 __device__ inline float soft_cap(float x, float cap, float inv)
 {
-    const float y = x * inv, y2 = y * y;
-    const float series = y * __builtin_fmaf(y2, __builtin_fmaf(y2, __builtin_fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+    const float y = x * inv;
     const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * kLog2e)) + 1.0f);
-    return cap * (fabsf(y) < 0.3f ? series : t);
+    return cap * (fabsf(y) < kTanhSeries ? tanh_series(y) : t);
 }
 
 // ONE: one part per sequence, eight wavefronts, and no merge afterwards.
