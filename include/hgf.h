@@ -232,7 +232,7 @@ hgf_status hgf_diff_attention_decode(const void *q_f16, const void *k_cache_f16,
  *   softcap      0 (none) or 1e-20 .. 1e20
  *   slopes       fp32 [2 n_heads] (device) or NULL: a distance bias per head of q, of magnitudes up to 1e30
  *   out_f16      fp16 [Tq, n_heads, d_h]; rows in front of cu_q[0] and behind cu_q[B] are left as they are
- * d_h 16, 32, 64 or 128; n_heads <= 1024; Tq, Tk < 2^24.  fp32 scores and sums; the softmax weights are
+ * d_h 16, 32, 64 or 128; B 1 .. 16384; n_heads 1 .. 1024; Tq, Tk 1 .. 2^24 - 1.  fp32 scores and sums; the softmax weights are
  * rounded to fp16 for the matrix cores.  What a row does not see does not change it, infinities and what is not a
  * number in k and v included. */
 hgf_status hgf_diff_attention_prefill(const void *q_f16, const void *k_f16, const void *v_f16, const int32_t *cu_q,
@@ -275,7 +275,7 @@ typedef struct {
 } hgf_kv8_cache;
 
 /* The operations on pages run on the device; new pages go to the requests in the order of their list, always the
- * free one with the lowest number.  `seqs`, `src`, `dst`: int32 [n] sequence numbers (n <= 16384); ok_out int32 [n] receives 1, or
+ * free one with the lowest number.  `seqs`, `src`, `dst`: int32 [n] sequence numbers (n 1 .. 16384); ok_out int32 [n] receives 1, or
  * 0 where a request was refused and changed nothing: a sequence outside 0 .. n_seqs-1 or one that the list names before
  * (as seqs or dst), or not enough free pages left for it and those before it (requests that need none are still granted).
  *
@@ -300,12 +300,13 @@ hgf_status hgf_kv8_pages_compact(const hgf_kv8_pages *pages, int32_t *pairs_out,
 /* Copies the contents (codes and scales) of page pairs[i][0] to page pairs[i][1], i < min(n, *count) (count NULL: n; both
  * on the device).  Pairs with a number outside 0 .. n_pages-1, or with twice the same one, are passed over.  No page
  * may be the destination of two pairs, or the source of one and the destination of another: such a page's contents are
- * not defined afterwards. */
+ * not defined afterwards.  n 1 .. 2^24. */
 hgf_status hgf_kv8_copy_pages(const hgf_kv8_cache *cache, const int32_t *pairs, const int32_t *count, int n, void *stream);
 
-/* In the calls below row b of the batch is sequence seqs[b] (int32 [B] on the device; NULL: sequence b, B <= n_seqs); rows whose
- * number lies outside 0 .. n_seqs-1 are passed over.  lens beyond the table are clipped to it, and positions whose page
- * number lies outside 0 .. n_pages-1 are not there: nothing is written to them, they are not attended to and read as zero.
+/* In the calls below row b of the batch is sequence seqs[b] (int32 [B] on the device, B 1 .. 16384; NULL: sequence b, B <= n_seqs);
+ * rows whose number lies outside 0 .. n_seqs-1 are passed over (by the attention: their outputs are zero).  T 1 .. 2^24 - 1.  lens
+ * beyond the table are clipped to it, and positions whose page number lies outside 0 .. n_pages-1 are not there: nothing is
+ * written to them, they are not attended to and read as zero.
  *
  * append: the new tokens of row b are the last ones of its sequence, positions lens - n .. lens - 1 (so the sequence
  *   has been grown before); k_f16 [T, 2 n_heads, d_h], v_f16 [T, n_heads, d_h] hold them in rows cu_new[b] .. cu_new[b+1]-1
@@ -320,7 +321,8 @@ hgf_status hgf_kv8_gather(const hgf_kv8_cache *cache, const hgf_kv8_pages *pages
 
 /* hgf_diff_attention_decode over such a cache: the newest token (position lens - 1, already appended) of every row attends to
  * all positions of its sequence, with the softcap and slopes of hgf_diff_attention_prefill (|p - j| = lens - 1 - j).
- *   q_f16     fp16 [B, 2 n_heads, d_h]       out_f16 fp16 [B, n_heads, d_h]; rows without positions become zero
+ *   q_f16     fp16 [B, 2 n_heads, d_h]       out_f16 fp16 [B, n_heads, d_h]; rows without positions become zero, whatever q
+ *             holds; else a head whose q (of either branch) holds an infinity or what is not a number is not a number
  *   workspace hgf_diff_attention_kv8_workspace_bytes(B, pages, n_heads, d_h) bytes, 16-byte aligned (0 bytes: may be NULL)
  * The products are exact (q and the softmax weights as 23-bit fixed-point numbers against the codes in the integer matrix
  * cores), statistics and sums are fp32. */

@@ -14,14 +14,18 @@
 // Weights are relative to the running maximum in base 2 and carried 2^7 larger, so that fp16 holds them down to
 // 2^-31; a row's maximum is only raised when a tile exceeds it by 2^8 (which the factor leaves room for), which spares
 // most rescalings.  fp32: scores, weights before rounding, sums, outputs.  The sum adds up the rounded weights.
+// The weights' rounding to fp16 leaves outputs 2.2e-4 to 2.6e-4 of their size (root mean square) off the result in 64 bits, of
+// which rounding the outputs themselves is 2.1e-4.  With what the rounding leaves as a second product that is all there is, but 4096
+// rows of 32 heads of 64 columns take 267 us in place of 182, three turns of 128 columns 206 in place of 177.
 // Masks are one comparison per element, key < limit of the row, and a comparison of document numbers where documents are
 // given, both only in tiles that need them; tiles whose document numbers lie outside those of the rows are not
 // read.  What a row does not see has weight 0; values of V that are no finite numbers are taken out of the tile and
 // added to the rows that see them (0 * inf would reach the others).
-// Bound by the chip's power limit: with two wavefronts to a SIMD a pass of 4096 rows, 32 heads of 64 columns took 404 000 clocks
-// at 1.97 GHz, with four 340 000 at 1.74 GHz, and taking out any part (staging, matrix instructions, exponentials) saves
-// about that part's time alone.  184 to 195 us by the card, 745 TFLOP/s (770 without causality, 865 with 128 columns), against 1350 of a
-// plain matrix product of 8192.
+// Bound by vector instructions, at the clock that the chip's power limit leaves: of the 340 000 clocks of a pass of 4096 rows, 32 heads
+// of 64 columns, the vector units issue in 237 000 (12 instructions to a matrix instruction) and the matrix cores are busy in 132 000,
+// at 1.74 GHz; with two wavefronts to a SIMD in place of four it was 404 000 clocks at 1.97 GHz, and taking out any part (staging,
+// matrix instructions, exponentials) saves about that part's time alone.  181 to 195 us by the card, 758 TFLOP/s (770 without
+// causality, 865 with 128 columns), against 1350 of a plain matrix product of 8192.
 #include "hgf_kv8.h"
 
 #include <limits.h>
