@@ -14,6 +14,8 @@
 // Weights are relative to the running maximum in base 2 and carried 2^7 larger, so that fp16 holds them down to
 // 2^-31; a row's maximum is only raised when a tile exceeds it by 2^8 (which the factor leaves room for), which spares
 // most rescalings.  fp32: scores, weights before rounding, sums, outputs.  The sum adds up the rounded weights.
+// A lane adds its keys up one step after the other: over four million random keys outputs stay within their rounding to fp16, over a
+// million equal ones behind a first key that outweighs them all together they are off by up to 1.4e-3.
 // The weights' rounding to fp16 leaves outputs 2.2e-4 to 2.6e-4 of their size (root mean square) off the result in 64 bits, of
 // which rounding the outputs themselves is 2.1e-4.  With what the rounding leaves as a second product that is all there is, but 4096
 // rows of 32 heads of 64 columns take 267 us in place of 182, three turns of 128 columns 206 in place of 177.
